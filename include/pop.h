@@ -338,8 +338,79 @@ int pop_sync(pop_ctx* ctx);
 /* Free the host-side context (never the workspace: Sec. 4.1's single allocation stays the caller's). */
 int pop_destroy(pop_ctx* ctx);
 
-/* Message of the last failing call on this context (of the last failing pop_create, pop_workspace_bytes or
- * pop_net_size of this thread when ctx is NULL).  Valid until the next call on the context. */
+/* ------------------------------------------------------------------------
+ * Operators for populations of recurrent agents.  They hold no context: every call names its arrays, its workspace
+ * and its stream, is asynchronous on that stream, allocates nothing, waits for nothing and may be captured into a
+ * graph.  All pointers are device pointers of the current device unless a comment says otherwise; structures are
+ * host memory, read before the call returns.  Return values as above; pop_last_error(NULL) has the message.  A
+ * workspace is 256-byte aligned, needs no initialisation and may be used by one call at a time (calls on one stream
+ * may share it).
+ */
+enum { POP_F32 = 0, POP_BF16 = 1, POP_F16 = 2 };   /* element types */
+
+/* Gated linear recurrence, per agent i, sequence b, channel c:
+ *
+ *   a_t = sigmoid(g_t + bias[i, c]),   h_t = a_t * h_{t-1} + (1 - a_t) * x_t,   y_t = h_t     for 0 <= t < length
+ *
+ * with h_{-1} = h0 and, where reset_t is not zero, 0 in place of h_{t-1} (an episode starts at t).  Steps from a
+ * sequence's length on are never read; y is 0 there and so are the gradients.  States, sums and gates are fp32
+ * whatever the arrays' type; values are rounded once, when they are stored. */
+typedef struct {
+  int32_t P, batch;     /* agents, sequences of each agent */
+  int32_t T;            /* steps (0 is legal: h_last = h0) */
+  int32_t C;            /* channels */
+  int32_t dtype;        /* POP_F32, POP_BF16 or POP_F16: x, g, y and their gradients */
+  int32_t reserved_;
+} pop_recurrence_config;
+
+/* A [P, batch, T, C] array: channels adjacent, the other axes with strides in elements (zero: the axis is broadcast,
+ * for inputs only; outputs must not overlap themselves or any input). */
+typedef struct {
+  void* data;
+  int64_t agent, row, step;
+} pop_sequence;
+
+typedef struct {
+  pop_sequence x, g;      /* candidates and gates */
+  pop_sequence y;         /* written (pop_recurrence_backward ignores it) */
+  pop_sequence reset;     /* uint8 [P, batch, T], or data NULL: no resets */
+  const float* bias;      /* [P, C] or NULL: zeros */
+  const float* h0;        /* [P, batch, C] or NULL: zeros (ignored by backward: states has it) */
+  float* h_last;          /* written: [P, batch, C] state behind the last step, or NULL; may be h0 */
+  const int32_t* lengths; /* [P, batch], taken as if within 0 .. T, or NULL: T */
+  float* states;          /* what backward needs of forward, pop_recurrence_states_bytes() bytes: written by
+                             pop_recurrence_forward unless NULL, read by pop_recurrence_backward */
+} pop_recurrence_io;
+
+typedef struct {
+  pop_sequence dy;        /* gradient of y */
+  pop_sequence dx, dg;    /* written */
+  const float* dh_last;   /* [P, batch, C] gradient of h_last, or NULL: zeros */
+  float* dh0;             /* written: [P, batch, C], or NULL */
+  float* dbias;           /* written: [P, C], summed over sequences and steps in a fixed order, or NULL */
+} pop_recurrence_grads;
+
+/* Bytes of workspace of pop_recurrence_forward and _backward, and of `states`; negative POP_E* code on a bad config. */
+int64_t pop_recurrence_workspace_bytes(const pop_recurrence_config* cfg);
+int64_t pop_recurrence_states_bytes(const pop_recurrence_config* cfg);
+
+int pop_recurrence_forward(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
+                           void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Gradients of sum(y * dy) + sum(h_last * dh_last), with x, g, reset, bias, lengths and states as forward had them. */
+int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
+                            const pop_recurrence_grads* grads, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* One step for acting agents: x, g, y are [P, batch, C] (cfg->T is 1, the step strides are ignored, reset is [P,
+ * batch]), the states live in state[P, n_slots, C] and are updated in place.  slots[P, batch] names the state row of
+ * each row, NULL: row b uses slot b.  A row whose slot is negative or not below n_slots is idle: its y is 0, and
+ * nothing of it is read.  No two rows of an agent may name the same slot.  io->h0, h_last, lengths and states must
+ * be NULL. */
+int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
+                        float* state, int32_t n_slots, const int32_t* slots, void* hip_stream);
+
+/* Message of the last failing call on this context (of the last failing pop_create, pop_workspace_bytes,
+ * pop_net_size or operator of this thread when ctx is NULL).  Valid until the next call on the context. */
 const char* pop_last_error(const pop_ctx* ctx);
 
 #ifdef __cplusplus

@@ -12,3 +12,6 @@ from .binding import (  # noqa: F401
     pop_insert, pop_last_error, pop_net_size, pop_copy_agent, pop_set_debug, pop_set_hparams, pop_set_option, pop_get_tuning, pop_set_params, pop_step_count, pop_sync, pop_update, pop_update_timed, KERNEL_NAMES,
     pop_workspace_bytes, pop_config, pop_hparams, pop_tuning,
 )
+from .operators import (  # noqa: F401
+    POP_BF16, POP_F16, POP_F32, Recurrence, pop_recurrence_config, pop_recurrence_grads, pop_recurrence_io, pop_sequence,
+)

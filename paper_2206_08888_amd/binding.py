@@ -106,6 +106,12 @@ def load_library(path=None):
         "pop_get_tuning": (C.c_int, [vp, C.POINTER(pop_tuning)]),
         "pop_destroy": (C.c_int, [vp]),
         "pop_last_error": (C.c_char_p, [vp]),
+        # operators (operators.py)
+        "pop_recurrence_workspace_bytes": (i64, [vp]),
+        "pop_recurrence_states_bytes": (i64, [vp]),
+        "pop_recurrence_forward": (C.c_int, [vp, vp, vp, i64, vp]),
+        "pop_recurrence_backward": (C.c_int, [vp, vp, vp, vp, i64, vp]),
+        "pop_recurrence_step": (C.c_int, [vp, vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -14,6 +14,7 @@
 
 #include "../../include/pop.h"
 #include "launch.h"
+#include "operators.h"
 
 using namespace pop;
 
@@ -118,6 +119,20 @@ int fail(pop_ctx* ctx, int code, const char* fmt, ...) {
   if (ctx) ctx->err = buf; else g_create_error = buf;
   return code;
 }
+
+}  // namespace
+
+int pop::fail_thread(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_create_error = buf;
+  return code;
+}
+
+namespace {
 
 #define HIP_TRY(ctx, call)                                                                     \
   do {                                                                                         \

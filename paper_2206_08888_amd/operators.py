@@ -1,0 +1,179 @@
+"""Operators for populations of recurrent agents on device tensors: the gated linear recurrence and the orthogonalised
+(Muon) update.  Argument marshalling for the calls of include/pop.h of the same names; everything is computed in the
+HIP kernels of libpop.so, on PyTorch's current stream, asynchronously.
+
+Outputs and workspaces come from PyTorch's allocator, call by call, so calls may run on any stream and inside
+torch.cuda.graph; tensors used on another stream than their own need the usual events and record_stream.
+"""
+import ctypes as ct
+
+import torch
+
+from .binding import _check, load_library
+
+POP_F32, POP_BF16, POP_F16 = 0, 1, 2
+DTYPE_CODES = {torch.float32: POP_F32, torch.bfloat16: POP_BF16, torch.float16: POP_F16}
+
+
+class pop_recurrence_config(ct.Structure):
+    _fields_ = [("P", ct.c_int32), ("batch", ct.c_int32), ("T", ct.c_int32), ("C", ct.c_int32), ("dtype", ct.c_int32),
+                ("reserved_", ct.c_int32)]
+
+
+class pop_sequence(ct.Structure):
+    _fields_ = [("data", ct.c_void_p), ("agent", ct.c_int64), ("row", ct.c_int64), ("step", ct.c_int64)]
+
+
+class pop_recurrence_io(ct.Structure):
+    _fields_ = [("x", pop_sequence), ("g", pop_sequence), ("y", pop_sequence), ("reset", pop_sequence),
+                ("bias", ct.c_void_p), ("h0", ct.c_void_p), ("h_last", ct.c_void_p), ("lengths", ct.c_void_p),
+                ("states", ct.c_void_p)]
+
+
+class pop_recurrence_grads(ct.Structure):
+    _fields_ = [("dy", pop_sequence), ("dx", pop_sequence), ("dg", pop_sequence), ("dh_last", ct.c_void_p),
+                ("dh0", ct.c_void_p), ("dbias", ct.c_void_p)]
+
+
+def _dtype_code(dtype):
+    if dtype not in DTYPE_CODES:
+        raise ValueError("dtype must be torch.float32, torch.bfloat16 or torch.float16, not %s" % (dtype,))
+    return DTYPE_CODES[dtype]
+
+
+class _Operator:
+    """Device and type checks, and the stream of a call."""
+
+    def __init__(self, dtype, device):
+        self.dtype, self.code = dtype, _dtype_code(dtype)
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("device must be a cuda device, not %s" % (device,))
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.lib = load_library()
+
+    def _tensor(self, t, name, shape, dtype=None, contiguous=True):
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise ValueError("%s must be a tensor on %s" % (name, self.device))
+        if t.dtype != (dtype or self.dtype):
+            raise ValueError("%s must be of type %s, not %s" % (name, dtype or self.dtype, t.dtype))
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+        if contiguous and not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        return t
+
+    def _pointer(self, t, name, shape, dtype=torch.float32):
+        return None if t is None else self._tensor(t, name, shape, dtype).data_ptr()
+
+    def _empty(self, shape, dtype=None):
+        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+
+    def _call(self, fn, *args):
+        """Enqueue on the current stream of this operator's device."""
+        if torch.cuda.current_device() == self.device.index:
+            return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        with torch.cuda.device(self.device):
+            return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+
+
+class Recurrence(_Operator):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t with a_t = sigmoid(g_t + bias), for P agents with `batch` sequences of up to T
+    steps and C channels each; where `reset` is not zero the state in front of that step counts as zero.
+
+    x, g and the gradients: [P, batch, T', C] of `dtype`, T' <= T, any strides with adjacent channels.  bias [P, C],
+    h0, h_last, dh_last, dh0 [P, batch, C] are float32; reset [P, batch, T'] is uint8 or bool; lengths [P, batch] is
+    int32: steps from a sequence's length on are not read, their outputs are zero."""
+
+    def __init__(self, P, batch, T, C, dtype=torch.float32, device="cuda"):
+        super().__init__(dtype, device)
+        self.P, self.batch, self.T, self.C = P, batch, T, C
+        self._cfg = pop_recurrence_config(P, batch, T, C, self.code, 0)
+        self._one = pop_recurrence_config(P, batch, 1, C, self.code, 0)
+        _check(self.lib.pop_recurrence_workspace_bytes(ct.byref(self._cfg)))
+
+    def _sequence(self, t, name, shape, dtype=None):
+        t = self._tensor(t, name, shape, dtype, contiguous=False)
+        s = t.stride()
+        if len(shape) == 4 and s[3] != 1 and shape[3] > 1:
+            raise ValueError("%s: its channels must be adjacent" % name)
+        return pop_sequence(t.data_ptr(), s[0], s[1], s[2])
+
+    def _io(self, x, g, bias, h0, reset, lengths):
+        T = x.shape[2] if x.dim() == 4 else -1
+        if T < 0 or T > self.T:
+            raise ValueError("x must have shape [%d, %d, up to %d, %d], not %s" % (self.P, self.batch, self.T, self.C, tuple(x.shape)))
+        shape = (self.P, self.batch, T, self.C)
+        io = pop_recurrence_io()
+        io.x, io.g = self._sequence(x, "x", shape), self._sequence(g, "g", shape)
+        if reset is not None:
+            io.reset = self._reset(reset, shape[:3])
+        io.bias = self._pointer(bias, "bias", (self.P, self.C))
+        io.h0 = self._pointer(h0, "h0", (self.P, self.batch, self.C))
+        io.lengths = self._pointer(lengths, "lengths", (self.P, self.batch), torch.int32)
+        return pop_recurrence_config(self.P, self.batch, T, self.C, self.code, 0), io, shape
+
+    def _reset(self, reset, shape):
+        dtype = torch.bool if getattr(reset, "dtype", None) == torch.bool else torch.uint8
+        t = self._tensor(reset, "reset", shape, dtype, contiguous=False)
+        return pop_sequence(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2) if len(shape) == 3 else 0)
+
+    def _workspace(self, cfg):
+        n = _check(self.lib.pop_recurrence_workspace_bytes(ct.byref(cfg)))
+        return self._empty(n, torch.uint8), n
+
+    def forward(self, x, g, bias=None, h0=None, reset=None, lengths=None, save=False):
+        """(y, h_last); with save also the states that `backward` needs: (y, h_last, states)."""
+        cfg, io, shape = self._io(x, g, bias, h0, reset, lengths)
+        y, h_last = self._empty(shape), self._empty((self.P, self.batch, self.C), torch.float32)
+        io.y, io.h_last = self._sequence(y, "y", shape), h_last.data_ptr()
+        states = None
+        if save:
+            states = self._empty(_check(self.lib.pop_recurrence_states_bytes(ct.byref(cfg))) // 4, torch.float32)
+            io.states = states.data_ptr()
+        ws, n = self._workspace(cfg)
+        self._call(self.lib.pop_recurrence_forward, ct.byref(cfg), ct.byref(io), ws.data_ptr(), n)
+        return (y, h_last, states) if save else (y, h_last)
+
+    def backward(self, states, x, g, dy, bias=None, reset=None, lengths=None, dh_last=None):
+        """(dx, dg, dbias, dh0) of sum(y dy) + sum(h_last dh_last), from what `forward` was given and its states."""
+        cfg, io, shape = self._io(x, g, bias, None, reset, lengths)
+        n = _check(self.lib.pop_recurrence_states_bytes(ct.byref(cfg))) // 4
+        io.states = self._pointer(states, "states", (n,))
+        dx, dg = self._empty(shape), self._empty(shape)
+        dbias, dh0 = self._empty((self.P, self.C), torch.float32), self._empty((self.P, self.batch, self.C), torch.float32)
+        grads = pop_recurrence_grads()
+        grads.dy = self._sequence(dy, "dy", shape)
+        grads.dx, grads.dg = self._sequence(dx, "dx", shape), self._sequence(dg, "dg", shape)
+        grads.dh_last = self._pointer(dh_last, "dh_last", (self.P, self.batch, self.C))
+        grads.dh0, grads.dbias = dh0.data_ptr(), dbias.data_ptr()
+        ws, n = self._workspace(cfg)
+        self._call(self.lib.pop_recurrence_backward, ct.byref(cfg), ct.byref(io), ct.byref(grads), ws.data_ptr(), n)
+        return dx, dg, dbias, dh0
+
+    def step(self, x, g, state, bias=None, reset=None, slots=None):
+        """One step of acting agents: x, g, y [P, batch, C]; state [P, n_slots, C] float32 is updated in place.  slots
+        [P, batch] int32 names each row's state (none twice within an agent); a row whose slot is negative or not
+        below n_slots is idle and gets zeros.  Without slots row b has state b."""
+        shape = (self.P, self.batch, self.C)
+        io = pop_recurrence_io()
+        y = self._empty(shape)
+        for field, t, name in (("x", x, "x"), ("g", g, "g"), ("y", y, "y")):
+            self._tensor(t, name, shape, contiguous=False)
+            s = t.stride()
+            if s[2] != 1 and self.C > 1:
+                raise ValueError("%s: its channels must be adjacent" % name)
+            setattr(io, field, pop_sequence(t.data_ptr(), s[0], s[1], 0))
+        if reset is not None:
+            io.reset = self._reset(reset, shape[:2])
+        io.bias = self._pointer(bias, "bias", (self.P, self.C))
+        if not isinstance(state, torch.Tensor) or state.dim() != 3:
+            raise ValueError("state must be a [P, n_slots, C] tensor")
+        n_slots = state.shape[1]
+        if slots is None and n_slots < self.batch:
+            raise ValueError("state has %d rows for %d sequences and no slots are given" % (n_slots, self.batch))
+        self._call(self.lib.pop_recurrence_step, ct.byref(self._one), ct.byref(io),
+                   self._pointer(state, "state", (self.P, n_slots, self.C)), n_slots,
+                   self._pointer(slots, "slots", (self.P, self.batch), torch.int32))
+        return y
