@@ -409,6 +409,58 @@ int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurren
 int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
                         float* state, int32_t n_slots, const int32_t* slots, void* hip_stream);
 
+/* Orthogonalised updates.  For a matrix G of r x c, with |G| its Frobenius norm:
+ *
+ *   X = G / (|G| + eps);   `steps` times:  A = X X^T,  X = k0 X + (k1 A + k2 A A) X         (Newton-Schulz products)
+ *
+ * which drives the singular values of G towards 1.  All sums are fp32 (|G|: fp64).  Products run on the fp16 matrix
+ * instructions from operands split into two halves of 11 bits each, which is fp32's precision up to the last bits. */
+enum { POP_NS_MAX_STEPS = 16 };
+typedef struct {
+  int32_t steps;                        /* 0 .. POP_NS_MAX_STEPS */
+  float eps;                            /* 1e-30 .. 1e30 */
+  float coef[POP_NS_MAX_STEPS][3];      /* k0, k1, k2 of every step.  POP_EUNSUPPORTED where they let singular values
+                                           of at most 1 grow beyond 8 */
+} pop_ns_config;
+
+/* `count` matrices of one shape: rows are `row` elements apart, matrices `matrix` elements, columns adjacent. */
+typedef struct {
+  void* data;
+  int64_t matrix, row;
+} pop_matrices;
+
+int64_t pop_orthogonalize_workspace_bytes(int32_t count, int32_t rows, int32_t cols);
+
+/* out = the orthogonalised g, both of type dtype; out may be g (with the same strides), else they must not overlap. */
+int pop_orthogonalize(const pop_ns_config* cfg, int32_t count, int32_t rows, int32_t cols, int32_t dtype,
+                      const pop_matrices* g, const pop_matrices* out,
+                      void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* The weight matrices of one layer of all agents ([P, rows, cols] each), for pop_muon_step. */
+typedef struct {
+  int32_t rows, cols;
+  float scale;             /* factor of the layer's update, e.g. sqrt(max(1, cols / rows)) for weights [in, out] */
+  int32_t reserved_;
+  pop_matrices grad;       /* of the call's dtype; read */
+  pop_matrices momentum;   /* float, updated */
+  pop_matrices weight;     /* float, updated */
+} pop_muon_layer;
+
+/* Hyperparameters of one agent; the population's lie in device memory, in stream order like every other array. */
+typedef struct { float lr, momentum, weight_decay; } pop_muon_hparams;
+
+/* Most layers of one call. */
+enum { POP_MUON_MAX_LAYERS = 8 };
+
+/* Bytes of workspace for layers of these shapes (only rows and cols are read). */
+int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_layer* layers);
+
+/* One optimiser step of every matrix of every agent (the Muon optimiser):
+ *   M = mu M + G;   U = nesterov ? G + mu M : M;   W = (1 - lr wd) W - lr scale O,   O = U orthogonalised. */
+int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype,
+                  int32_t nesterov, const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes,
+                  void* hip_stream);
+
 /* Message of the last failing call on this context (of the last failing pop_create, pop_workspace_bytes,
  * pop_net_size or operator of this thread when ctx is NULL).  Valid until the next call on the context. */
 const char* pop_last_error(const pop_ctx* ctx);

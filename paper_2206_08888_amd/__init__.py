@@ -13,5 +13,6 @@ from .binding import (  # noqa: F401
     pop_workspace_bytes, pop_config, pop_hparams, pop_tuning,
 )
 from .operators import (  # noqa: F401
-    POP_BF16, POP_F16, POP_F32, Recurrence, pop_recurrence_config, pop_recurrence_grads, pop_recurrence_io, pop_sequence,
+    POP_BF16, POP_F16, POP_F32, Muon, NS_COEF, Orthogonalizer, Recurrence, make_ns_config, pop_matrices, pop_muon_layer, pop_ns_config,
+    pop_recurrence_config, pop_recurrence_grads, pop_recurrence_io, pop_sequence,
 )

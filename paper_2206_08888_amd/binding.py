@@ -112,6 +112,10 @@ def load_library(path=None):
         "pop_recurrence_forward": (C.c_int, [vp, vp, vp, i64, vp]),
         "pop_recurrence_backward": (C.c_int, [vp, vp, vp, vp, i64, vp]),
         "pop_recurrence_step": (C.c_int, [vp, vp, vp, i32, vp, vp]),
+        "pop_orthogonalize_workspace_bytes": (i64, [i32, i32, i32]),
+        "pop_orthogonalize": (C.c_int, [vp, i32, i32, i32, i32, vp, vp, vp, i64, vp]),
+        "pop_muon_workspace_bytes": (i64, [i32, i32, vp]),
+        "pop_muon_step": (C.c_int, [vp, i32, i32, vp, i32, i32, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

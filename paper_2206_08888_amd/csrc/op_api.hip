@@ -11,6 +11,8 @@ constexpr int64_t kAlignment = 256;          // of a workspace
 constexpr int64_t kMaxLanes = 1ll << 31;     // a launch's work items per grid dimension stay below 2^32
 constexpr int kMaxSteps = 1 << 22;           // chunks of a sequence are a grid dimension of at most 65,535
 
+constexpr double kMostSingular = 8.0;
+
 int64_t element_bytes(int32_t dtype) { return dtype == POP_F32 ? 4 : 2; }
 
 int check_recurrence(const pop_recurrence_config* c) {
@@ -61,6 +63,75 @@ int check_workspace(void* p, int64_t have, int64_t need) {
   if ((uintptr_t)p % kAlignment) return fail_thread(POP_EINVAL, "workspace must be 256-byte aligned");
   if (have < need) return fail_thread(POP_ENOMEM, "workspace has %lld bytes, %lld needed", (long long)have, (long long)need);
   return POP_OK;
+}
+
+// NsCall::most and gain.  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
+// in s^2; p(s) / s at an end or where its derivative in s^2 is 0.
+void bounds_of(const pop_ns_config& c, NsCall& n) {
+  double top = 1.0, gain = 1.0;
+  n.most = 1.0f;
+  for (int k = 0; k < c.steps; ++k) {
+    n.gain[k] = (float)fmin(gain, 1e30);
+    const double k0 = c.coef[k][0], k1 = c.coef[k][1], k2 = c.coef[k][2], end = top * top;
+    const auto ratio = [&](double q) { return fabs(k0 + k1 * q + k2 * q * q); };             // q = s^2
+    double next = ratio(end) * top, most = fmax(ratio(0.0), ratio(end));
+    const auto turn = [&](double q) { if (q > 0.0 && q < end) next = fmax(next, ratio(q) * sqrt(q)); };
+    const double d = 9 * k1 * k1 - 20 * k0 * k2;
+    if (k2 != 0.0 && d >= 0.0) { turn((-3 * k1 + sqrt(d)) / (10 * k2)); turn((-3 * k1 - sqrt(d)) / (10 * k2)); }
+    if (k2 == 0.0 && k1 != 0.0) turn(-k0 / (3 * k1));
+    if (k2 != 0.0 && -k1 / (2 * k2) > 0.0 && -k1 / (2 * k2) < end) most = fmax(most, ratio(-k1 / (2 * k2)));
+    top = next;
+    gain *= most;
+    n.most = (float)fmax(n.most, top);
+    if (!(n.most <= kMostSingular)) return;
+  }
+  n.gain[c.steps] = (float)fmin(gain, 1e30);
+}
+
+int check_ns(const pop_ns_config* c, int32_t dtype, NsCall& n) {
+  if (!c) return fail_thread(POP_EINVAL, "config is NULL");
+  if (c->steps < 0 || c->steps > POP_NS_MAX_STEPS) return fail_thread(POP_EINVAL, "steps must be 0 .. %d", (int)POP_NS_MAX_STEPS);
+  if (!(c->eps >= 1e-30f && c->eps <= 1e30f)) return fail_thread(POP_EINVAL, "eps must be within 1e-30 .. 1e30");
+  if (dtype != POP_F32 && dtype != POP_BF16 && dtype != POP_F16) return fail_thread(POP_EINVAL, "unknown dtype %d", dtype);
+  for (int k = 0; k < c->steps; ++k)
+    for (float v : c->coef[k])
+      if (!isfinite(v)) return fail_thread(POP_EINVAL, "coefficients of step %d are not finite", k);
+  n = NsCall{};
+  bounds_of(*c, n);
+  if (!(n.most <= kMostSingular)) return fail_thread(POP_EUNSUPPORTED, "the coefficients let singular values of at most 1 grow beyond %g", kMostSingular);
+  n.steps = c->steps;
+  n.eps = c->eps;
+  for (int k = 0; k < c->steps; ++k)
+    for (int i = 0; i < 3; ++i) n.coef[k][i] = c->coef[k][i];
+  return POP_OK;
+}
+
+int check_shape(int64_t count, int64_t rows, int64_t cols) {
+  if (count < 1 || rows < 1 || cols < 1) return fail_thread(POP_EINVAL, "a matrix count, rows or cols is not positive");
+  if (rows > kNsMaxSide || cols > kNsMaxSide) return fail_thread(POP_EUNSUPPORTED, "rows and cols must be at most %d", kNsMaxSide);
+  // workgroups take at least a 32 x 32 block; a launch has fewer than 2^24 of them
+  if (count * ((rows + 31) / 32) * ((cols + 31) / 32) >= 1 << 20) return fail_thread(POP_EUNSUPPORTED, "more than 2^20 blocks of 32 x 32 in %lld matrices", (long long)count);
+  return POP_OK;
+}
+
+int check_matrices(int64_t count, int64_t rows, int64_t cols, const pop_matrices& m, const char* name, bool output, int64_t bytes) {
+  if (!m.data) return fail_thread(POP_EINVAL, "%s is NULL", name);
+  if ((uintptr_t)m.data % bytes) return fail_thread(POP_EINVAL, "%s is not aligned to its type", name);
+  const int64_t n[2] = {count, rows}, stride[2] = {m.matrix, m.row};
+  if (output && !apart(cols, 2, n, stride)) return fail_thread(POP_EINVAL, "%s: its strides let elements overlap", name);
+  return POP_OK;
+}
+
+int64_t muon_workspace(int32_t P, int32_t n_layers, const pop_muon_layer* layers) {
+  if (n_layers < 1 || n_layers > POP_MUON_MAX_LAYERS) return fail_thread(POP_EINVAL, "n_layers must be 1 .. %d", (int)POP_MUON_MAX_LAYERS);
+  if (!layers) return fail_thread(POP_EINVAL, "layers is NULL");
+  int64_t sum = 0;
+  for (int k = 0; k < n_layers; ++k) {
+    const int rc = check_shape(P, layers[k].rows, layers[k].cols);
+    if (rc != POP_OK) return rc;
+    sum += ns_workspace_bytes(P, layers[k].rows, layers[k].cols);
+  }
+  return sum;
 }
 
 int launched(hipError_t e) { return e == hipSuccess ? POP_OK : fail_thread(POP_EHIP, "kernel launch: %s", hipGetErrorString(e)); }
@@ -155,6 +226,63 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
   if (n_slots < 1) return fail_thread(POP_EINVAL, "n_slots must be positive");
   a.state = state; a.n_slots = n_slots; a.slots = slots;
   return launched(launch_recur_step(a, cfg->dtype, (hipStream_t)hip_stream));
+}
+
+int64_t pop_orthogonalize_workspace_bytes(int32_t count, int32_t rows, int32_t cols) {
+  const int rc = check_shape(count, rows, cols);
+  return rc != POP_OK ? rc : ns_workspace_bytes(count, rows, cols);
+}
+
+int pop_orthogonalize(const pop_ns_config* cfg, int32_t count, int32_t rows, int32_t cols, int32_t dtype, const pop_matrices* g,
+                      const pop_matrices* out, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  NsCall n;
+  int rc = check_ns(cfg, dtype, n);
+  if (rc != POP_OK || (rc = check_shape(count, rows, cols)) != POP_OK) return rc;
+  if (!g || !out) return fail_thread(POP_EINVAL, "g or out is NULL");
+  if ((rc = check_matrices(count, rows, cols, *g, "g", false, element_bytes(dtype))) != POP_OK ||
+      (rc = check_matrices(count, rows, cols, *out, "out", true, element_bytes(dtype))) != POP_OK)
+    return rc;
+  if (g->data == out->data && (g->matrix != out->matrix || g->row != out->row))
+    return fail_thread(POP_EINVAL, "out may be g only with the same strides");
+  if ((rc = check_workspace(workspace, workspace_bytes, ns_workspace_bytes(count, rows, cols))) != POP_OK) return rc;
+  n.n_layers = 1;
+  NsLayer& l = n.layer[0];
+  l.rows = rows; l.cols = cols; l.count = count;
+  l.g = g->data; l.g_matrix = g->matrix; l.g_row = g->row;
+  l.out = out->data; l.out_matrix = out->matrix; l.out_row = out->row;
+  return launched(launch_ns(n, dtype, workspace, (hipStream_t)hip_stream));
+}
+
+int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_layer* layers) { return muon_workspace(P, n_layers, layers); }
+
+int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype, int32_t nesterov,
+                  const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  NsCall n;
+  int rc = check_ns(cfg, dtype, n);
+  if (rc != POP_OK) return rc;
+  const int64_t need = muon_workspace(P, n_layers, layers);
+  if (need < 0) return (int)need;
+  if ((rc = check_floats(hparams, "hparams", true)) != POP_OK) return rc;
+  n.n_layers = n_layers;
+  n.nesterov = nesterov != 0;
+  n.hparams = (const float*)hparams;
+  for (int k = 0; k < n_layers; ++k) {
+    const pop_muon_layer& m = layers[k];
+    if ((rc = check_matrices(P, m.rows, m.cols, m.grad, "grad", false, element_bytes(dtype))) != POP_OK ||
+        (rc = check_matrices(P, m.rows, m.cols, m.momentum, "momentum", true, 4)) != POP_OK ||
+        (rc = check_matrices(P, m.rows, m.cols, m.weight, "weight", true, 4)) != POP_OK)
+      return rc;
+    if (!isfinite(m.scale)) return fail_thread(POP_EINVAL, "layer %d: scale is not finite", k);
+    if (m.momentum.data == m.weight.data || m.grad.data == m.weight.data || m.grad.data == m.momentum.data)
+      return fail_thread(POP_EINVAL, "layer %d: grad, momentum and weight must not overlap", k);
+    NsLayer& l = n.layer[k];
+    l.rows = m.rows; l.cols = m.cols; l.count = P; l.scale = m.scale;
+    l.g = m.grad.data; l.g_matrix = m.grad.matrix; l.g_row = m.grad.row;
+    l.momentum = (float*)m.momentum.data; l.m_matrix = m.momentum.matrix; l.m_row = m.momentum.row;
+    l.weight = (float*)m.weight.data; l.w_matrix = m.weight.matrix; l.w_row = m.weight.row;
+  }
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  return launched(launch_ns(n, dtype, workspace, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

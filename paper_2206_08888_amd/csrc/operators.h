@@ -37,4 +37,31 @@ hipError_t launch_recur_forward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_backward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_step(const RecurArgs& a, int dtype, hipStream_t s);
 
+
+// ---- orthogonalised updates
+
+constexpr int kNsMaxSide = 16384;
+
+struct NsLayer {                     // matrices of one shape
+  int rows, cols, count;
+  const void* g;                     // gradients, or the matrices to orthogonalise
+  int64_t g_matrix, g_row;
+  void* out;                         // orthogonalised matrices, of g's type; or NULL and
+  int64_t out_matrix, out_row;
+  float *momentum, *weight;          // momenta and weights to update
+  int64_t m_matrix, m_row, w_matrix, w_row;
+  float scale;
+};
+struct NsCall {
+  int n_layers, steps, nesterov;
+  float eps;
+  const float* hparams;              // [count, 3] learning rate, momentum, weight decay; NULL: no momentum
+  float coef[POP_NS_MAX_STEPS][3];
+  float most;                        // singular values that start within [0, 1] stay below this in every step,
+  float gain[POP_NS_MAX_STEPS + 1];  // and within gain[k] of what they started from in front of step k
+  NsLayer layer[POP_MUON_MAX_LAYERS];
+};
+int64_t ns_workspace_bytes(int count, int rows, int cols);      // of one layer, a multiple of 256
+hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s);
+
 }  // namespace pop

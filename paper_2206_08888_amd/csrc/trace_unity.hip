@@ -21,6 +21,7 @@ __device__ unsigned long long g_pop_block_time[kTraceKinds][2][kTraceBlocks];
 #include "k_sac.hip"
 #include "k_wgrad_shared.hip"
 #include "k_recurrence.hip"
+#include "k_orthogonalize.hip"
 #include "pop_api.hip"
 #include "op_api.hip"
 

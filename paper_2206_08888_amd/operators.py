@@ -35,6 +35,34 @@ class pop_recurrence_grads(ct.Structure):
                 ("dh0", ct.c_void_p), ("dbias", ct.c_void_p)]
 
 
+NS_MAX_STEPS, MUON_MAX_LAYERS = 16, 8
+NS_COEF = (3.4445, -4.7750, 2.0315)                      # five steps take singular values of 0.01 .. 1 to 0.7 .. 1.2
+
+
+class pop_ns_config(ct.Structure):
+    _fields_ = [("steps", ct.c_int32), ("eps", ct.c_float), ("coef", (ct.c_float * 3) * NS_MAX_STEPS)]
+
+
+class pop_matrices(ct.Structure):
+    _fields_ = [("data", ct.c_void_p), ("matrix", ct.c_int64), ("row", ct.c_int64)]
+
+
+class pop_muon_layer(ct.Structure):
+    _fields_ = [("rows", ct.c_int32), ("cols", ct.c_int32), ("scale", ct.c_float), ("reserved_", ct.c_int32),
+                ("grad", pop_matrices), ("momentum", pop_matrices), ("weight", pop_matrices)]
+
+
+def make_ns_config(steps=5, coef=NS_COEF, eps=1e-7):
+    """coef: (k0, k1, k2) for all steps, or one such triple per step."""
+    cfg = pop_ns_config(steps, eps)
+    each = [coef] * steps if not coef or not hasattr(coef[0], "__len__") else list(coef)
+    if len(each) != steps or any(len(k) != 3 for k in each):
+        raise ValueError("coef must be three numbers, or three for each of %d steps" % steps)
+    for k in range(min(steps, NS_MAX_STEPS)):
+        cfg.coef[k][:] = each[k]
+    return cfg
+
+
 def _dtype_code(dtype):
     if dtype not in DTYPE_CODES:
         raise ValueError("dtype must be torch.float32, torch.bfloat16 or torch.float16, not %s" % (dtype,))
@@ -177,3 +205,68 @@ class Recurrence(_Operator):
                    self._pointer(state, "state", (self.P, n_slots, self.C)), n_slots,
                    self._pointer(slots, "slots", (self.P, self.batch), torch.int32))
         return y
+
+
+class _NewtonSchulz(_Operator):
+    def _matrices(self, t, name, shape, dtype=None):
+        t = self._tensor(t, name, shape, dtype, contiguous=False)
+        s = t.stride()
+        if s[2] != 1 and shape[2] > 1:
+            raise ValueError("%s: its columns must be adjacent" % name)
+        return pop_matrices(t.data_ptr(), s[0], s[1])
+
+
+class Orthogonalizer(_NewtonSchulz):
+    """orthogonalizer(g): Newton-Schulz products drive the singular values of every matrix of g [count, rows, cols]
+    towards 1 (the products an orthogonalised optimiser takes its updates through).  Any strides with adjacent columns."""
+
+    def __init__(self, count, rows, cols, dtype=torch.float32, device="cuda", steps=5, coef=NS_COEF, eps=1e-7):
+        super().__init__(dtype, device)
+        self.shape = (count, rows, cols)
+        self._ns = make_ns_config(steps, coef, eps)
+        self._bytes = _check(self.lib.pop_orthogonalize_workspace_bytes(count, rows, cols))
+
+    def __call__(self, g, out=None):
+        """A new tensor, or `out` (which may be g)."""
+        out = self._empty(self.shape) if out is None else out
+        gm, om = self._matrices(g, "g", self.shape), self._matrices(out, "out", self.shape)
+        ws = self._empty(self._bytes, torch.uint8)
+        self._call(self.lib.pop_orthogonalize, ct.byref(self._ns), *self.shape, self.code, ct.byref(gm), ct.byref(om),
+                   ws.data_ptr(), self._bytes)
+        return out
+
+
+class Muon(_NewtonSchulz):
+    """One optimiser step for the weight matrices of P agents, layer by layer [P, rows, cols]:
+
+      M = mu M + G;  U = G + mu M (nesterov) or M;  W = (1 - lr wd) W - lr scale O,  O = U orthogonalised
+
+    Weights and momenta are float32, gradients of `dtype`; any strides with adjacent columns.  shapes: (rows, cols) of
+    each layer (at most 8); scales: a factor of each layer's update, by default sqrt(max(1, cols / rows)) (weights are
+    [in, out])."""
+
+    def __init__(self, P, shapes, dtype=torch.float32, device="cuda", scales=None, nesterov=True, steps=5, coef=NS_COEF, eps=1e-7):
+        super().__init__(dtype, device)
+        self.P, self.shapes, self.nesterov = P, [tuple(s) for s in shapes], nesterov
+        scales = [max(1.0, c / r) ** 0.5 for r, c in self.shapes] if scales is None else list(scales)
+        if len(scales) != len(self.shapes):
+            raise ValueError("%d scales for %d layers" % (len(scales), len(self.shapes)))
+        self._ns = make_ns_config(steps, coef, eps)
+        self._layers = (pop_muon_layer * max(1, len(self.shapes)))()
+        for l, (r, c), f in zip(self._layers, self.shapes, scales):
+            l.rows, l.cols, l.scale = r, c, f
+        self._bytes = _check(self.lib.pop_muon_workspace_bytes(P, len(self.shapes), self._layers))
+
+    def step(self, weights, momenta, grads, hparams):
+        """weights, momenta (both updated in place), grads: one tensor per layer.  hparams: float32 tensor [P, 3] on the
+        device, learning rate, momentum and weight decay of every agent."""
+        if not len(weights) == len(momenta) == len(grads) == len(self.shapes):
+            raise ValueError("weights, momenta and grads must have %d tensors each" % len(self.shapes))
+        layers = (pop_muon_layer * len(self.shapes)).from_buffer_copy(self._layers)
+        for l, (r, c), w, m, g in zip(layers, self.shapes, weights, momenta, grads):
+            shape = (self.P, r, c)
+            l.weight, l.momentum = self._matrices(w, "weight", shape, torch.float32), self._matrices(m, "momentum", shape, torch.float32)
+            l.grad = self._matrices(g, "grad", shape)
+        ws = self._empty(self._bytes, torch.uint8)
+        self._call(self.lib.pop_muon_step, ct.byref(self._ns), self.P, len(self.shapes), layers, self.code, int(self.nesterov),
+                   self._pointer(hparams, "hparams", (self.P, 3)), ws.data_ptr(), self._bytes)

@@ -129,3 +129,62 @@ def test_recurrence_step_refuses(lib, kw):
     assert call(one, _io(), None, 3) == pp.POP_EINVAL
     assert call(one, _io(), ADDRESS + 2, 3) == pp.POP_EINVAL
     assert call(one, _io(), ADDRESS, 0) == pp.POP_EINVAL
+
+
+@pytest.mark.parametrize("name", ["pop_ns_config", "pop_matrices", "pop_muon_layer"])
+def test_structures_of_orthogonalised_updates_match_the_header(lib, tmp_path, name):
+    test_structures_match_the_header(lib, tmp_path, name)
+
+
+def _orthogonalize(lib, cfg=None, count=2, rows=5, cols=6, dtype=pp.POP_F32, g=(ADDRESS, 30, 6), out=(2 * ADDRESS, 30, 6),
+                   ws=3 * ADDRESS, size=1 << 40):
+    ref = lambda s: None if s is None else C.byref(ops.pop_matrices(*s))
+    return lib.pop_orthogonalize(C.byref(cfg or pp.make_ns_config()), count, rows, cols, dtype, ref(g), ref(out), ws, size, None)
+
+
+def _ns(**kw):
+    cfg = pp.make_ns_config()
+    for k, v in kw.items():
+        setattr(cfg, k, v)
+    return cfg
+
+
+@pytest.mark.parametrize("kw, code", [
+    (dict(count=0), pp.POP_EINVAL), (dict(rows=0), pp.POP_EINVAL), (dict(cols=-1), pp.POP_EINVAL), (dict(dtype=7), pp.POP_EINVAL),
+    (dict(rows=16385), pp.POP_EUNSUPPORTED), (dict(cols=16385), pp.POP_EUNSUPPORTED), (dict(count=1 << 20), pp.POP_EUNSUPPORTED),
+    (dict(g=None), pp.POP_EINVAL), (dict(out=None), pp.POP_EINVAL), (dict(g=(None, 30, 6)), pp.POP_EINVAL),
+    (dict(g=(ADDRESS + 2, 30, 6)), pp.POP_EINVAL), (dict(out=(ADDRESS, 30, 6), g=(ADDRESS, 60, 6)), pp.POP_EINVAL),
+    (dict(out=(2 * ADDRESS, 0, 6)), pp.POP_EINVAL), (dict(out=(2 * ADDRESS, 30, 5)), pp.POP_EINVAL), (dict(out=(2 * ADDRESS, 6, 6)), pp.POP_EINVAL),
+    (dict(ws=None), pp.POP_EINVAL), (dict(ws=ADDRESS + 64), pp.POP_EINVAL), (dict(size=100), pp.POP_ENOMEM),
+    (dict(cfg=_ns(steps=-1)), pp.POP_EINVAL), (dict(cfg=_ns(steps=17)), pp.POP_EINVAL), (dict(cfg=_ns(eps=0.0)), pp.POP_EINVAL),
+    (dict(cfg=_ns(eps=float("nan"))), pp.POP_EINVAL)])
+def test_orthogonalize_refuses(lib, kw, code):
+    assert _orthogonalize(lib, **kw) == code
+    assert pp.pop_last_error(None) != ""
+
+
+@pytest.mark.parametrize("coef, code", [((float("nan"), 0, 0), pp.POP_EINVAL), ((9.0, 0.0, 0.0), pp.POP_EUNSUPPORTED),
+                                        ((3.0, 0.0, 0.0), pp.POP_EUNSUPPORTED), ((1.5, 0.5, 0.0), pp.POP_EUNSUPPORTED),
+                                        ((1.0, 30.0, -31.0), pp.POP_EUNSUPPORTED), ((1e30, 1e30, 1e30), pp.POP_EUNSUPPORTED)])
+def test_coefficients_that_let_singular_values_grow_are_refused(lib, coef, code):
+    """(1, 30, -31): 0 and 1 stay, what lies between grows to 8.3 and beyond."""
+    assert _orthogonalize(lib, cfg=pp.make_ns_config(5, coef)) == code
+
+
+def test_muon_refuses(lib):
+    def call(P=2, n=1, dtype=pp.POP_F32, hp=5 * ADDRESS, ws=4 * ADDRESS, size=1 << 40, none=False, **kw):
+        layers = (ops.pop_muon_layer * 9)()
+        for l in layers:
+            l.rows, l.cols, l.scale = 5, 6, 1.0
+            l.grad, l.momentum, l.weight = (ops.pop_matrices(k * ADDRESS, 30, 6) for k in (1, 2, 3))
+        for k, v in kw.items():
+            setattr(layers[0], k, v)
+        return lib.pop_muon_step(C.byref(pp.make_ns_config()), P, n, None if none else layers, dtype, 1, hp, ws, size, None)
+
+    for kw in (dict(P=0), dict(n=0), dict(n=9), dict(none=True), dict(dtype=-1), dict(hp=None), dict(hp=ADDRESS + 1), dict(ws=None), dict(rows=0),
+               dict(scale=float("inf")), dict(weight=ops.pop_matrices(2 * ADDRESS, 30, 6)), dict(grad=ops.pop_matrices(3 * ADDRESS, 30, 6)),
+               dict(momentum=ops.pop_matrices(None, 30, 6)), dict(weight=ops.pop_matrices(3 * ADDRESS, 0, 6)),
+               dict(grad=ops.pop_matrices(ADDRESS + 1, 30, 6))):
+        assert call(**kw) == pp.POP_EINVAL, kw
+    assert call(size=100) == pp.POP_ENOMEM
+    assert call(rows=20000) == pp.POP_EUNSUPPORTED
