@@ -2,14 +2,25 @@
 //
 //   X = U / (|U| + eps);  steps times:  A = X X^T,  B = k1 A + k2 A A,  X = k0 X + B X
 //
-// with X of m x n, m <= n (matrices with more rows than columns are taken transposed).  All matrices of a call advance
-// together: per step one launch for A, one for B, one for X; A and B are symmetric, so only their tiles on and above
-// the diagonal are computed.
+// with X of m x n, m <= n (matrices with more rows than columns are taken transposed).  The steps multiply X by
+// polynomials of A, which commute, so several of them are taken in the space of A: with P = k0 + B,
+//
+//   A = X X^T;  per step:  Q = P Q,  A = P A P;  then X = Q X
+//
+// where every product is of two commuting symmetric m x m matrices, half of whose tiles are computed.  X (m x n) is
+// touched twice per segment of steps instead of twice per step.  An error of A grows by up to k0^2 per step there, where
+// a step on X starts from a fresh A: segments of kNsSegment = 3 steps (errors against 64 bits over 256 x 256, 256 x 1024,
+// 64 x 2048 gradients 7e-7, 1.0e-6, 5e-7; all five steps in one segment 9e-6, 6e-7, 4e-7, and 3e-3 for a 31 x 32 gradient
+// with one small singular value; each step on X 2.7e-7; fp32 products 1.7e-6, 2.1e-6, 1.2e-6).
+//
+// All matrices of a call advance together, a launch per product.  Layers whose m is at most 64 do all products of a
+// segment that are m x m in one workgroup.
 //
 // Products on v_mfma_f32_32x32x16_f16 from operands in two fp16 halves, x = hi + lo with 11 bits each, held in units
 // (powers of two, Units below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
-// entries down to 2^-14 of the largest: x y = hi hi + hi lo + lo hi, what is left out is below 2^-22 |x y|.  Three instructions in
-// place of sixteen of the fp32 ones.
+// entries down to 2^-14 of the largest: x y = hi hi + hi lo + lo hi, what is left out is below 2^-22 |x y|.  Three
+// instructions in place of sixteen of the fp32 ones.  The matrix pipe rounds its accumulator after every instruction: the
+// two small products have one of their own, so that a sum is rounded a third as often.
 //
 // Operands lie in the workspace as the instruction takes them: blocks of 32 rows x 16 contraction indices, 64 lanes
 // of 8 halves (lane l: row l & 31, indices 8 (l >> 5) ..), the hi block in front of the lo block, 2 KB together,
@@ -22,339 +33,696 @@ namespace {
 namespace ns {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPair = 1024;                 // halves of a hi and a lo block
+constexpr int kSmall = 2;                   // bands of m up to which one workgroup does a segment's m x m products
 
 // Where the arrays of one matrix lie, in halves from the start of its workspace.
 struct Place {
   int mb, nb;                               // 32-row bands of m and n
-  int64_t x, xt[2], a, b, size;             // X [m rows, n inside], X^T [n rows, m inside] twice, A, B
+  int64_t x, xt[2], a, b, t, q[2], size;    // X [m rows, n inside], X^T [n rows, m inside] twice; A, B, P A, Q twice
 };
-__host__ __device__ inline Place place(int rows, int cols) {
+__host__ __device__ inline Place place(int mb, int nb) {
   Place p;
-  p.mb = ((rows < cols ? rows : cols) + 31) / 32;
-  p.nb = ((rows < cols ? cols : rows) + 31) / 32;
-  const int64_t xs = (int64_t)p.mb * p.nb * 2 * kPair, as = (int64_t)p.mb * p.mb * 2 * kPair;
-  p.x = 0; p.xt[0] = xs; p.xt[1] = 2 * xs; p.a = 3 * xs; p.b = 3 * xs + as;
-  p.size = 3 * xs + 2 * as;
+  p.mb = mb;
+  p.nb = nb;
+  const int64_t xs = (int64_t)mb * nb * 2 * kPair, as = (int64_t)mb * mb * 2 * kPair;
+  p.x = 0; p.xt[0] = xs; p.xt[1] = 2 * xs;
+  p.a = 3 * xs; p.b = p.a + as; p.t = p.b + as; p.q[0] = p.t + as; p.q[1] = p.q[0] + as;
+  p.size = p.q[1] + as;
   return p;
 }
+__host__ __device__ inline Place place_of(int rows, int cols) {
+  return place(((rows < cols ? rows : cols) + 31) / 32, ((rows < cols ? cols : rows) + 31) / 32);
+}
 constexpr int kSumParts = 256;              // most partial sums of one matrix's squares
-constexpr int kSums = kSumParts + 1;        // behind them |X| of the first X
-__host__ __device__ inline int64_t part_elements(int rows, int cols) {
+__host__ __device__ inline int part_elements(int rows, int cols) {
   const int64_t n = (int64_t)rows * cols, a = (n + kSumParts - 1) / kSumParts;
-  return a > 8192 ? a : 8192;
+  return (int)(a > 8192 ? a : 8192);
 }
 __host__ __device__ inline int parts(int rows, int cols) {
   const int64_t e = part_elements(rows, cols);
   return (int)(((int64_t)rows * cols + e - 1) / e);
 }
 
-__host__ __device__ inline int64_t sum_bytes(int count) { return ((int64_t)count * kSums * 8 + 255) / 256 * 256; }
-
-// Units of X, A = X X^T and B = k1 A + k2 A A in front of a step: powers of two by which entries are held multiplied.
-// No entry exceeds the largest singular value, which is below `most` whatever the matrix, and below gain[step] |X| of
-// the first X where eps made that small.  (The limits on the exponents keep the units and what they divide finite:
-// an X below 2^-100 is as good as none, and an A or B below 2^-60 makes no difference to X.)
-struct Units { float x, a, b; };
-__device__ inline float unit_of(float most, int limit) { return ldexpf(1.0f, min(14 - ilogbf(fmaxf(most, 0x1p-120f)), limit)); }
-__device__ inline Units units_of(const NsCall& c, int step, float start) {
-  const float x = fminf(c.most, start * c.gain[step]), a = x * x;
-  return {unit_of(x, 100), unit_of(a, 60), unit_of(fabsf(c.coef[step][1]) * a + fabsf(c.coef[step][2]) * a * a, 60)};
-}
-
-struct Work {                               // a launch: workgroups of every layer
-  int first[POP_MUON_MAX_LAYERS + 1];       // first workgroup of a layer
-  int per[POP_MUON_MAX_LAYERS];             // workgroups of one matrix
-  int64_t ws[POP_MUON_MAX_LAYERS];          // bytes to the layer's workspace
+// Factors of a step's products (two of each product, as one may not be finite) and of what is added to them.
+struct Factors { float p0, p1, old; };
+struct StepFactors {
+  float gram0, gram1;                       // A = X X^T
+  Factors poly, q, t, next;                 // B, Q (in a segment's first step: of B and of the unit matrix), T, A
+  float done0, done1;                       // X = Q X behind the step
+};
+// A matrix's workspace in front of its blocks.
+struct Head {
+  double sums[kSumParts];
+  StepFactors step[POP_NS_MAX_STEPS];
 };
 
-struct At { int layer, matrix, unit; };
-__device__ inline At find(const Work& w) {
-  int k = 0;
-  while ((int)blockIdx.x >= w.first[k + 1]) ++k;
-  const int i = (int)blockIdx.x - w.first[k];
-  return {k, i / w.per[k], i % w.per[k]};
+// ---- arguments of a launch: few lines, as each is a trip to memory where it is first used
+
+struct LayerArg {
+  int per, count, mb, nb;                   // workgroups of one matrix, matrices, bands
+  int64_t ws;                               // bytes to the layer's workspace
+  int64_t turned;                           // more rows than columns: X is the transpose
+};
+struct Args {
+  int first[POP_MUON_MAX_LAYERS];           // first workgroup of a layer, a multiple of 8
+  int step, first_step, last_step, parity, done_parity, xt;   // number, whether the segment's first, last; which Q, Q at its end, X^T
+  LayerArg layer[POP_MUON_MAX_LAYERS];
+};
+struct EndArg {                             // a caller's arrays of a layer
+  const void* g;
+  int64_t g_matrix, g_row;
+  float* m;
+  int64_t m_matrix, m_row;
+  void* out;                                // weights, or results
+  int64_t out_matrix, out_row;
+  int rows, cols;
+  float scale;
+  int reserved;
+};
+struct Ends {
+  const float* hparams;
+  float eps;
+  int nesterov;
+  EndArg layer[POP_MUON_MAX_LAYERS];
+};
+struct NoEnds {};
+
+// Units in front of a step of X and A = X X^T, of B = k1 A + k2 A A and of T = P A: powers of two by which entries are
+// held multiplied.  No entry exceeds the largest singular value.  That of X is below `most` whatever the matrix, and
+// below gain[step] |X| of the first X where eps made that small; T's are those of X times those of the next X; Q's are
+// bounded by the coefficients alone.  (The limits on the exponents keep the units and what they divide finite: an X
+// below 2^-100 is as good as none, and an A, B or T below 2^-60 makes no difference to X.)
+__device__ inline float unit_of(float most, int limit) {
+  const int e = 14 - ilogbf(fmaxf(most, 0x1p-120f));
+  return ldexpf(1.0f, e < limit ? e : limit);
+}
+struct Bounds {                             // NsCall
+  int steps;
+  float most, coef[POP_NS_MAX_STEPS][3], gain[POP_NS_MAX_STEPS + 1], q_most[POP_NS_MAX_STEPS];
+};
+__device__ inline float x_most(const Bounds& c, int step, float start) { return fminf(c.most, start * c.gain[step]); }
+__device__ inline StepFactors factors_of(const Bounds& c, int k, float start) {
+  const int first = k / kNsSegment * kNsSegment;
+  const float k0 = c.coef[k][0], k1 = c.coef[k][1], k2 = c.coef[k][2], most = x_most(c, k, start), after = x_most(c, k + 1, start), a2 = most * most;
+  const float x = unit_of(most, 100), a = unit_of(a2, 60), b = unit_of(fabsf(k1) * a2 + fabsf(k2) * a2 * a2, 60), t = unit_of(most * after, 60),
+              a_next = unit_of(after * after, 60), q = unit_of(c.q_most[k], 60);
+  StepFactors f;
+  f.gram0 = 1.0f / x; f.gram1 = a / x;
+  f.poly = {1.0f / a, k2 * (b / a), k1 * (b / a)};
+  if (k == first) f.q = {q / b, 1.0f, k0 * q};
+  else { const float before = unit_of(c.q_most[k - 1], 60); f.q = {1.0f / b, q / before, k0 * (q / before)}; }
+  f.t = {1.0f / b, t / a, k0 * (t / a)};
+  f.next = {1.0f / b, a_next / t, k0 * (a_next / t)};
+  f.done0 = 1.0f / q; f.done1 = (k + 1 == c.steps ? 1.0f : unit_of(after, 100)) / unit_of(x_most(c, first, start), 100);
+  return f;
 }
 
-// a layer's workspace: sums [count, kSums], then the matrices
-__device__ inline double* sums_of(char* ws, const Work& w, const At& at) { return (double*)(ws + w.ws[at.layer]) + (int64_t)at.matrix * kSums; }
-__device__ inline _Float16* halves_of(char* ws, const Work& w, const At& at, const NsLayer& l, const Place& p) {
-  return (_Float16*)(ws + w.ws[at.layer] + sum_bytes(l.count)) + (int64_t)at.matrix * p.size;
+// Workgroups go to the 8 XCDs in turn; from 8 matrices on all those of one matrix go to one XCD, whose L2 then reads
+// the matrix once.
+struct At { int layer, matrix, unit; LayerArg l; };
+__device__ inline At find(const Args& c) {
+  const int block = (int)blockIdx.x;
+  At at;
+  at.layer = 0;
+#pragma unroll
+  for (int k = 1; k < POP_MUON_MAX_LAYERS; ++k) at.layer += block >= c.first[k];
+  at.l = c.layer[at.layer];
+  const int i = block - c.first[at.layer], per = at.l.per, n = at.l.count < 8 ? i : i >> 3;
+  at.matrix = n / per;
+  at.unit = n - at.matrix * per;
+  if (at.l.count >= 8) at.matrix = at.matrix * 8 + (i & 7);
+  return at;
+}
+
+// a layer's workspace: the heads, then the matrices
+__host__ __device__ inline int64_t head_bytes(int count) { return ((int64_t)count * sizeof(Head) + 255) / 256 * 256; }
+__device__ inline Head& head_of(char* ws, const At& at) { return ((Head*)(ws + at.l.ws))[at.matrix]; }
+__device__ inline _Float16* halves_of(char* ws, const At& at, const Place& p) {
+  return (_Float16*)(ws + at.l.ws + head_bytes(at.l.count)) + (int64_t)at.matrix * p.size;
 }
 
 // ---- momentum and norms
 
 constexpr int kThreads = 256;
 
+__device__ inline double block_sum(double v, double* red) {
+  for (int s = 32; s > 0; s /= 2) v += __shfl_xor(v, s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
+}
+
 template <typename G>
-__global__ void __launch_bounds__(kThreads) k_norms(NsCall c, Work w, char* ws) {
-  __shared__ double red[kThreads];
-  const At at = find(w);
-  const NsLayer& l = c.layer[at.layer];
-  const int64_t e = part_elements(l.rows, l.cols), n = (int64_t)l.rows * l.cols;
-  const int64_t lo = at.unit * e, hi = lo + e < n ? lo + e : n;
-  const float mu = c.hparams ? c.hparams[3 * at.matrix + 1] : 0.0f;
+__global__ void __launch_bounds__(kThreads) k_norms(Args c, Ends ends, char* ws) {
+  __shared__ double red[4];
+  const At at = find(c);
+  const EndArg l = ends.layer[at.layer];
+  if (at.matrix >= at.l.count) return;
+  const int e = part_elements(l.rows, l.cols), n = l.rows * l.cols;
+  const int lo = at.unit * e, hi = min(lo + e, n);
+  const float mu = ends.hparams ? ends.hparams[3 * at.matrix + 1] : 0.0f;
+  const G* g = (const G*)l.g + at.matrix * l.g_matrix;
+  float* m = ends.hparams ? l.m + at.matrix * l.m_matrix : nullptr;
+  // rows without gaps are one run of elements
+  const bool flat = l.g_row == l.cols && (!m || l.m_row == l.cols);
   double sum = 0.0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const int r = (int)(i / l.cols), k = (int)(i % l.cols);
-    float u = (float)((const G*)l.g)[at.matrix * l.g_matrix + r * l.g_row + k];
-    if (c.hparams) {
-      float* m = l.momentum + at.matrix * l.m_matrix + r * l.m_row + k;
-      const float v = fmaf(mu, *m, u);
-      *m = v;
-      u = c.nesterov ? fmaf(mu, v, u) : v;
+#pragma unroll 8
+  for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
+    const int r = flat ? 0 : i / l.cols, k = flat ? i : i - r * l.cols;
+    float u = (float)g[r * l.g_row + k];
+    if (m) {
+      float* to = m + r * l.m_row + k;
+      const float v = fmaf(mu, *to, u);
+      *to = v;
+      u = ends.nesterov ? fmaf(mu, v, u) : v;
     }
     sum += (double)u * u;
   }
-  red[threadIdx.x] = sum;
-  __syncthreads();
-  for (int s = kThreads / 2; s > 0; s /= 2) {
-    if ((int)threadIdx.x < s) red[threadIdx.x] += red[threadIdx.x + s];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) sums_of(ws, w, at)[at.unit] = red[0];
+  sum = block_sum(sum, red);
+  if (threadIdx.x == 0) head_of(ws, at).sums[at.unit] = sum;
 }
 
 // |U| from the partial sums, the same in every workgroup
 __device__ inline double norm_of(const double* sums, int n, double* red) {
-  red[threadIdx.x] = (int)threadIdx.x < n ? sums[threadIdx.x] : 0.0;
-  __syncthreads();
-  for (int s = kThreads / 2; s > 0; s /= 2) {
-    if ((int)threadIdx.x < s) red[threadIdx.x] += red[threadIdx.x + s];
-    __syncthreads();
-  }
-  return sqrt(red[0]);
+  return sqrt(block_sum((int)threadIdx.x < n ? sums[threadIdx.x] : 0.0, red));
 }
 
 // ---- blocks of operands
 
 // Accumulator tile of 32 x 32: register 4 q + r of lane l is element (row i = 8 q + 4 (l >> 5) + r, column j = l & 31).
-// `put_turned` writes it with j as the row and i inside (four i are adjacent); `put` with i as the row and j inside, by
-// way of 32 x 33 words of LDS of this wavefront.  band: 32-row band of the target, inside: its 32 inner indices' number.
-struct Halves { _Float16 hi, lo; };
-__device__ inline Halves split(float v) {
-  const _Float16 hi = (_Float16)v;
-  return {hi, (_Float16)(v - (float)hi)};
+// `put_turned` writes registers 4 q .. of it with j as the row and i inside (four i are adjacent) to turned_at() +
+// turned(q); `put` with i as the row and j inside, by way of 32 x 36 words of LDS.  band: 32-row band of the target,
+// inside: its 32 inner indices' number.
+struct Quad { f16x4 hi, lo; };
+__device__ inline Quad split(const f32x4& v) {
+  Quad h;
+  h.hi = __builtin_convertvector(v, f16x4);
+  h.lo = __builtin_convertvector(v - __builtin_convertvector(h.hi, f32x4), f16x4);
+  return h;
 }
+__device__ inline f32x4 value(const Quad& p) { return __builtin_convertvector(p.hi, f32x4) + __builtin_convertvector(p.lo, f32x4); }
 __device__ inline int64_t pair_at(int band, int inside16, int bands_inside) { return ((int64_t)band * bands_inside * 2 + inside16) * kPair; }
-
-__device__ inline void put_turned(_Float16* base, int band, int inside, int bands_inside, const f32x16& v) {
+__device__ inline int64_t turned_at(int band, int inside, int bands_inside) {
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    f16x4 hi, lo;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const Halves h = split(v[4 * q + r]);
-      hi[r] = h.hi;
-      lo[r] = h.lo;
-    }
-    _Float16* to = base + pair_at(band, 2 * inside + (q >> 1), bands_inside) + ((lane & 31) + 32 * (q & 1)) * 8 + 4 * (lane >> 5);
-    *(f16x4*)to = hi;
-    *(f16x4*)(to + kPair / 2) = lo;
-  }
+  return pair_at(band, 2 * inside, bands_inside) + ((lane & 31) * 8 + 4 * (lane >> 5));
 }
-__device__ inline void put(_Float16* base, int band, int inside, int bands_inside, const f32x16& v, float* scratch) {
-  const int lane = threadIdx.x & 63;
-  __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int i = 0; i < 16; ++i) scratch[(8 * (i >> 2) + 4 * (lane >> 5) + (i & 3)) * 33 + (lane & 31)] = v[i];
-  __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    f16x8 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const Halves h = split(scratch[(lane & 31) * 33 + 16 * s + 8 * (lane >> 5) + i]);
-      hi[i] = h.hi;
-      lo[i] = h.lo;
-    }
-    _Float16* to = base + pair_at(band, 2 * inside + s, bands_inside) + lane * 8;
-    *(f16x8*)to = hi;
-    *(f16x8*)(to + kPair / 2) = lo;
-  }
-  __builtin_amdgcn_wave_barrier();
+__device__ constexpr int turned(int q) { return (q >> 1) * kPair + (q & 1) * 256; }
+__device__ inline void put_turned(_Float16* to, const Quad& v) {
+  *(f16x4*)to = v.hi;
+  *(f16x4*)(to + kPair / 2) = v.lo;
 }
-// what put_turned wrote
-__device__ inline f32x16 get_turned(const _Float16* base, int band, int inside, int bands_inside) {
+__device__ inline Quad get_turned(const _Float16* from) { return {*(const f16x4*)from, *(const f16x4*)(from + kPair / 2)}; }
+constexpr int kStride = 36;                 // words; 16-byte reads of 8 rows meet all banks
+__device__ inline void stage(unsigned* scratch, int q, const Quad& v) {
   const int lane = threadIdx.x & 63;
-  f32x16 v;
+  unsigned* to = scratch + (4 * (lane >> 5)) * kStride + (lane & 31) + 8 * q * kStride;
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 hi = __builtin_bit_cast(u32x2, v.hi), lo = __builtin_bit_cast(u32x2, v.lo);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const _Float16* from = base + pair_at(band, 2 * inside + (q >> 1), bands_inside) + ((lane & 31) + 32 * (q & 1)) * 8 + 4 * (lane >> 5);
-    const f16x4 hi = *(const f16x4*)from, lo = *(const f16x4*)(from + kPair / 2);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[4 * q + r] = (float)hi[r] + (float)lo[r];
-  }
-  return v;
+  for (int r = 0; r < 4; ++r) to[r * kStride] = __builtin_amdgcn_perm(lo[r >> 1], hi[r >> 1], r & 1 ? 0x07060302u : 0x05040100u);
+}
+__device__ inline void put(_Float16* to, const unsigned* scratch, int half) {        // to: pair_at(band, 2 * inside + half, ..)
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63;
+  const u32x4* from = (const u32x4*)(scratch + (lane & 31) * kStride + 16 * half + 8 * (lane >> 5));
+  const u32x4 a = from[0], b = from[1];
+  const u32x4 hi = {__builtin_amdgcn_perm(a[1], a[0], 0x05040100u), __builtin_amdgcn_perm(a[3], a[2], 0x05040100u),
+                    __builtin_amdgcn_perm(b[1], b[0], 0x05040100u), __builtin_amdgcn_perm(b[3], b[2], 0x05040100u)};
+  const u32x4 lo = {__builtin_amdgcn_perm(a[1], a[0], 0x07060302u), __builtin_amdgcn_perm(a[3], a[2], 0x07060302u),
+                    __builtin_amdgcn_perm(b[1], b[0], 0x07060302u), __builtin_amdgcn_perm(b[3], b[2], 0x07060302u)};
+  *(u32x4*)(to + lane * 8) = hi;
+  *(u32x4*)(to + lane * 8 + kPair / 2) = lo;
 }
 
 // ---- X in both orders
 
+// A lane's corner of block (ib, jb) of a caller's matrix; its register 4 q + r lies 8 q + r rows below.
+struct Corner {
+  int64_t at;                               // elements from the start of the array
+  int rows;                                 // rows of the matrix from the corner on (0: the column is outside)
+};
+__device__ inline Corner corner(int matrix, int64_t matrix_stride, int64_t row_stride, int rows, int cols, int ib, int jb) {
+  const int lane = threadIdx.x & 63, i = ib * 32 + 4 * (lane >> 5), j = jb * 32 + (lane & 31);
+  return {matrix * matrix_stride + i * row_stride + j, j < cols ? max(rows - i, 0) : 0};
+}
+
 template <typename G>
-__global__ void __launch_bounds__(kThreads) k_start(NsCall c, Work w, char* ws) {
-  __shared__ double red[kThreads];
-  __shared__ float scratch[4][32 * 33];
-  const At at = find(w);
-  const NsLayer& l = c.layer[at.layer];
-  const Place p = place(l.rows, l.cols);
-  double* sums = sums_of(ws, w, at);
-  const double norm = norm_of(sums, parts(l.rows, l.cols), red), inv = 1.0 / (norm + (double)c.eps);
-  const float start = (float)(norm * inv);
-  if (at.unit == 0 && threadIdx.x == 0) sums[kSumParts] = start;
-  const double scale = inv * units_of(c, 0, start).x;
-  const float mu = c.hparams ? c.hparams[3 * at.matrix + 1] : 0.0f;
-  const bool turned = l.rows > l.cols;
-  const int cb = turned ? p.mb : p.nb, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+__global__ void __launch_bounds__(kThreads) k_start(Args c, Bounds bounds, Ends ends, char* ws) {
+  __shared__ double red[4];
+  __shared__ __attribute__((aligned(16))) unsigned scratch[4][32 * kStride];
+  const At at = find(c);
+  const EndArg l = ends.layer[at.layer];
+  if (at.matrix >= at.l.count) return;
+  const Place p = place(at.l.mb, at.l.nb);
+  const float mu = ends.hparams ? ends.hparams[3 * at.matrix + 1] : 0.0f;
+  const bool turned_in = l.rows > l.cols, plain = !ends.hparams || ends.nesterov;
+  const int cb = turned_in ? p.mb : p.nb, wave = threadIdx.x >> 6;
   const int block = at.unit * 4 + wave;
-  if (block >= p.mb * p.nb) return;
+  const bool on = block < p.mb * p.nb;
   const int ib = block / cb, jb = block % cb;
-  f32x16 v;
+  float u[16], m[16];
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
-    const int r = ib * 32 + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3), j = jb * 32 + (lane & 31);
-    float u = 0.0f;
-    if (r < l.rows && j < l.cols) {
-      const bool plain = !c.hparams || c.nesterov;
-      const float g = plain ? (float)((const G*)l.g)[at.matrix * l.g_matrix + r * l.g_row + j] : 0.0f;
-      const float m = c.hparams ? l.momentum[at.matrix * l.m_matrix + r * l.m_row + j] : 0.0f;
-      u = (float)((double)(c.hparams ? (c.nesterov ? fmaf(mu, m, g) : m) : g) * scale);
-    }
-    v[k] = u;
+  for (int k = 0; k < 16; ++k) u[k] = m[k] = 0.0f;
+  if (plain) {
+    const Corner o = corner(at.matrix, l.g_matrix, l.g_row, on ? l.rows : 0, l.cols, ib, jb);
+    const G* from = (const G*)l.g + o.at;
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (8 * (k >> 2) + (k & 3) < o.rows) u[k] = (float)from[(8 * (k >> 2) + (k & 3)) * l.g_row];
   }
-  _Float16* base = halves_of(ws, w, at, l, p);
+  if (ends.hparams) {
+    const Corner o = corner(at.matrix, l.m_matrix, l.m_row, on ? l.rows : 0, l.cols, ib, jb);
+    const float* from = l.m + o.at;
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (8 * (k >> 2) + (k & 3) < o.rows) m[k] = from[(8 * (k >> 2) + (k & 3)) * l.m_row];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) u[k] = plain ? fmaf(mu, m[k], u[k]) : m[k];
+  }
+  Head& head = head_of(ws, at);
+  const double norm = norm_of(head.sums, parts(l.rows, l.cols), red), inv = 1.0 / (norm + (double)ends.eps);
+  const float start = (float)(norm * inv);
+  if (at.unit == 0 && (int)threadIdx.x < bounds.steps) head.step[threadIdx.x] = factors_of(bounds, threadIdx.x, start);
+  const double scale = inv * unit_of(x_most(bounds, 0, start), 100);
+  if (!on) return;
+  _Float16* base = halves_of(ws, at, p);
   // rows of the matrix are m unless it is turned
-  put_turned(base + (turned ? p.x : p.xt[0]), jb, ib, turned ? p.nb : p.mb, v);
-  put(base + (turned ? p.xt[0] : p.x), ib, jb, turned ? p.mb : p.nb, v, scratch[wave]);
+  _Float16* across = base + (turned_in ? p.x : p.xt[0]) + turned_at(jb, ib, turned_in ? p.nb : p.mb);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    f32x4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = (float)((double)u[4 * q + r] * scale);
+    const Quad h = split(v);
+    put_turned(across + turned(q), h);
+    stage(scratch[wave], q, h);
+  }
+  __builtin_amdgcn_wave_barrier();
+  _Float16* along = base + (turned_in ? p.xt[0] : p.x) + pair_at(ib, 2 * jb, turned_in ? p.mb : p.nb);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) put(along + half * kPair, scratch[wave], half);
 }
 
 // ---- products
 
-enum { kGram = 0, kPoly = 1, kApply = 2, kLast = 3 };
-constexpr int kTile = 4;                    // 32-row bands of a workgroup's tile: 2 x 2 wavefronts of 2 x 2 blocks
-
 __device__ inline f32x16 mfma(const f16x8& a, const f16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
+struct Pair { f16x8 hi, lo; };
+__device__ inline Pair load_pair(const _Float16* p) { return {*(const f16x8*)p, *(const f16x8*)(p + kPair / 2)}; }
+struct Acc {
+  f32x16 large, small;
+  __device__ inline void add(const Pair& l, const Pair& r) {
+    small = mfma(l.hi, r.lo, small);
+    large = mfma(l.hi, r.hi, large);
+    small = mfma(l.lo, r.hi, small);
+  }
+};
 
-template <int MODE, typename G>
-__global__ void __launch_bounds__(kThreads) k_product(NsCall c, Work w, char* ws, int step) {
-  __shared__ float scratch[4][32 * 33];
-  const At at = find(w);
-  const NsLayer& l = c.layer[at.layer];
-  const Place p = place(l.rows, l.cols);
-  const bool turned = MODE == kLast && l.rows > l.cols;
-  _Float16* base = halves_of(ws, w, at, l, p);
-  const _Float16 *xt = base + p.xt[step & 1];
-  // left operand: rows i, right operand: rows j, `inner` blocks of 16
-  const _Float16* left = MODE == kGram ? base + p.x : MODE == kPoly ? base + p.a : turned ? xt : base + p.b;
-  const _Float16* right = MODE == kGram ? base + p.x : MODE == kPoly ? base + p.a : turned ? base + p.b : xt;
-  const int ibands = turned ? p.nb : p.mb, jbands = MODE < kApply || turned ? p.mb : p.nb;
-  const int inner = 2 * (MODE == kGram ? p.nb : p.mb);
-  int ti, tj;
-  if (MODE < kApply) {                      // tiles on and above the diagonal
-    const int t = (p.mb + kTile - 1) / kTile;
-    ti = 0;
-    int u = at.unit;
-    while (u >= t - ti) { u -= t - ti; ++ti; }
-    tj = ti + u;
+// kGram: A = X X^T.  kPoly: B = k1 A + k2 A A, in the first step of a segment Q = k0 + B as well.  kMix: T = k0 A + B A
+// but in the last step of a segment, Q = k0 Q + B Q but in the first.  kNext: A = k0 T + B T.  kApply: X = Q X.  kLast:
+// the same, into the result.
+enum { kGram = 0, kPoly = 1, kMix = 2, kNext = 3, kApply = 4, kLast = 5 };
+
+__device__ inline void triangle(int t, int u, int& i, int& j) {       // entry u of the upper triangle of t x t tiles
+  i = 0;
+  while (u >= t - i) { u -= t - i; ++i; }
+  j = i + u;
+}
+__host__ __device__ inline int tiles(int t) { return t * (t + 1) / 2; }
+
+// One product of a launch: rows i of `left` times rows j of `right`, `inner` blocks of 16; what is added to it, k0 (kPoly:
+// k1) times `old`; where the result goes with j as the row, and its mirror image (kApply: X beside X^T).
+struct Product {
+  const _Float16 *left, *right, *old;
+  _Float16 *to, *mirror;
+  int ibands, jbands, inner;
+  bool turned, q_task;
+};
+// unit: the workgroup's number among those of its matrix; side: tiles or blocks along m.
+template <int MODE> __device__ inline Product product_of(const Args& c, const At& at, const Place& p, _Float16* base, int& unit, int side) {
+  Product o;
+  o.turned = MODE == kLast && at.l.turned;
+  o.q_task = MODE == kMix && (c.last_step || (!c.first_step && unit >= tiles(side)));
+  if (MODE == kMix && unit >= tiles(side)) unit -= tiles(side);
+  o.ibands = o.jbands = p.mb;
+  o.inner = 2 * p.mb;
+  o.old = o.to = o.mirror = nullptr;
+  _Float16 *q = base + p.q[c.parity], *q_before = base + p.q[c.parity ^ 1], *done = base + p.q[c.done_parity];
+  if (MODE == kGram) {
+    o.left = o.right = base + p.x;
+    o.to = o.mirror = base + p.a;
+    o.inner = 2 * p.nb;
+  } else if (MODE == kPoly) {
+    o.left = o.right = o.old = base + p.a;
+    o.to = o.mirror = base + p.b;
+  } else if (MODE == kMix) {
+    o.left = base + p.b;
+    o.right = o.old = o.q_task ? q_before : base + p.a;
+    o.to = o.mirror = o.q_task ? q : base + p.t;
+  } else if (MODE == kNext) {
+    o.left = base + p.b;
+    o.right = o.old = base + p.t;
+    o.to = o.mirror = base + p.a;
+  } else if (o.turned) {
+    o.left = base + p.xt[c.xt];
+    o.right = done;
+    o.ibands = p.nb;
   } else {
-    const int t = (jbands + kTile - 1) / kTile;
-    ti = at.unit / t;
-    tj = at.unit % t;
+    o.left = done;
+    o.right = base + p.xt[c.xt];
+    o.jbands = p.nb;
+    o.to = base + p.xt[c.xt ^ 1];
+    o.mirror = base + p.x;
   }
+  return o;
+}
+template <int MODE> __device__ inline Factors factors_of(const StepFactors& f, bool q_task) {
+  if (MODE == kGram) return {f.gram0, f.gram1, 0.0f};
+  if (MODE == kPoly) return f.poly;
+  if (MODE == kMix) return q_task ? f.q : f.t;
+  if (MODE == kNext) return f.next;
+  return {f.done0, f.done1, 0.0f};
+}
+// The first step's Q = k0 + B, from values of B.
+__device__ inline f32x4 first_q(const Factors& f, int ib, int jb, int q, const f32x4& b) {
+  const int lane = threadIdx.x & 63, i = 8 * q + 4 * (lane >> 5), j = ib == jb ? lane & 31 : -1;
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = fmaf(b[r], f.p0, i + r == j ? f.old : 0.0f);
+  return v;
+}
+
+// Registers 4 q .. of a block of results: weights are read ahead of the product, written behind it.
+template <int MODE, typename E> __device__ inline f32x4 read_weights(const E& ends, const At& at, int ib, int jb, int q) {
+  f32x4 w = {};
+  if constexpr (MODE == kLast) {
+    if (ends.hparams) {
+      const EndArg& l = ends.layer[at.layer];
+      const Corner c = corner(at.matrix, l.out_matrix, l.out_row, l.rows, l.cols, ib, jb);
+      const float* from = (const float*)l.out + c.at;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (8 * q + r < c.rows) w[r] = from[(8 * q + r) * l.out_row];
+    }
+  }
+  return w;
+}
+template <typename G> __device__ inline void write_result(const Ends& ends, const At& at, int ib, int jb, int q, const f32x4& w, const f32x4& v) {
+  const EndArg& l = ends.layer[at.layer];
+  const Corner c = corner(at.matrix, l.out_matrix, l.out_row, l.rows, l.cols, ib, jb);
+  if (ends.hparams) {
+    const float* hp = ends.hparams + 3 * at.matrix;
+    const float up = -hp[0] * l.scale, keep = fmaf(-hp[0], hp[2], 1.0f);
+    float* to = (float*)l.out + c.at;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (8 * q + r < c.rows) to[(8 * q + r) * l.out_row] = fmaf(up, v[r], w[r] * keep);
+  } else {
+    G* to = (G*)l.out + c.at;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (8 * q + r < c.rows) to[(8 * q + r) * l.out_row] = (G)v[r];
+  }
+}
+
+// One 32 x 32 block per workgroup; the wavefronts take a quarter of the contraction each, then a quarter of the block.
+template <int MODE, typename G, typename E>
+__global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
+  __shared__ float part[4][16][64];
+  __shared__ __attribute__((aligned(16))) unsigned scratch[32 * kStride];
+  const At at = find(c);
+  if (at.matrix >= at.l.count) return;
+  const Place p = place(at.l.mb, at.l.nb);
+  _Float16* base = halves_of(ws, at, p);
+  int unit = at.unit, ib, jb;
+  const Product o = product_of<MODE>(c, at, p, base, unit, p.mb);
+  if (MODE < kApply) triangle(p.mb, unit, ib, jb);
+  else { ib = unit / o.jbands; jb = unit - ib * o.jbands; }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int i0 = ti * kTile + (wave >> 1) * 2, j0 = tj * kTile + (wave & 1) * 2;
-  if (i0 >= ibands || j0 >= jbands) return;
-  const _Float16 *lp[2], *rp[2];
+  const int q4 = (o.inner + 3) / 4, lo = wave * q4, hi = min(lo + q4, o.inner);
+  const _Float16 *lp = o.left + (int64_t)ib * o.inner * kPair + lane * 8, *rp = o.right + (int64_t)jb * o.inner * kPair + lane * 8;
+  Acc acc = {};
+  int k = lo;
+  const StepFactors& step = head_of(ws, at).step[c.step];
+  const Factors f = factors_of<MODE>(step, o.q_task), fq = step.q;
+  const int64_t place_to = turned_at(jb, ib, p.mb) + turned(wave);
+  Quad old = {};
+  if (o.old) old = get_turned(o.old + place_to);
+  const f32x4 weights = read_weights<MODE>(ends, at, ib, jb, wave);
+  for (; k + 4 <= hi; k += 4) {
+    Pair x[4], y[4];
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {             // a band beyond the edge: the last one again, not stored
-    lp[s] = left + (int64_t)min(i0 + s, ibands - 1) * inner * kPair + lane * 8;
-    rp[s] = right + (int64_t)min(j0 + s, jbands - 1) * inner * kPair + lane * 8;
+    for (int i = 0; i < 4; ++i) { x[i] = load_pair(lp + (int64_t)(k + i) * kPair); y[i] = load_pair(rp + (int64_t)(k + i) * kPair); }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc.add(x[i], y[i]);
   }
-  f32x16 acc[2][2] = {};
-  for (int k = 0; k < inner; ++k) {
-    f16x8 lh[2], ll[2], rh[2], rl[2];
+  for (; k < hi; ++k) acc.add(load_pair(lp + (int64_t)k * kPair), load_pair(rp + (int64_t)k * kPair));
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      lh[s] = *(const f16x8*)(lp[s] + (int64_t)k * kPair);
-      ll[s] = *(const f16x8*)(lp[s] + (int64_t)k * kPair + kPair / 2);
-      rh[s] = *(const f16x8*)(rp[s] + (int64_t)k * kPair);
-      rl[s] = *(const f16x8*)(rp[s] + (int64_t)k * kPair + kPair / 2);
+  for (int i = 0; i < 16; ++i) part[wave][i][lane] = acc.large[i] + acc.small[i];
+  __syncthreads();
+  const f32x4 before = value(old);
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = 4 * wave + r;
+    v[r] = ((part[0][i][lane] + part[1][i][lane]) + (part[2][i][lane] + part[3][i][lane])) * f.p0 * f.p1 + before[r] * f.old;
+  }
+  if constexpr (MODE == kLast) {
+    write_result<G>(ends, at, ib, jb, wave, weights, v);
+  } else {
+    Quad h = split(v);
+    put_turned(o.to + place_to, h);
+    const bool mirrored = MODE == kApply || ib != jb;
+    const int64_t mirror_to = pair_at(ib, 2 * jb + wave, MODE == kApply ? p.nb : p.mb);
+    if (mirrored) {
+      stage(scratch, wave, h);
+      __syncthreads();
+      if (wave < 2) put(o.mirror + mirror_to, scratch, wave);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        acc[i][j] = mfma(lh[i], rl[j], acc[i][j]);
-        acc[i][j] = mfma(ll[i], rh[j], acc[i][j]);
-        acc[i][j] = mfma(lh[i], rh[j], acc[i][j]);
+    if (MODE == kPoly && c.first_step) {
+      h = split(first_q(fq, ib, jb, wave, v));
+      put_turned(base + p.q[0] + place_to, h);
+      if (mirrored) {
+        __syncthreads();
+        stage(scratch, wave, h);
+        __syncthreads();
+        if (wave < 2) put(base + p.q[0] + mirror_to, scratch, wave);
       }
+    }
   }
-  const float start = (float)sums_of(ws, w, at)[kSumParts];
-  const Units u = units_of(c, step, start);
-  const float next = MODE == kLast ? 1.0f : units_of(c, step + 1, start).x;
-  const float k0 = c.coef[step][0], k1 = c.coef[step][1], k2 = c.coef[step][2];
+}
+
+// Tiles of 128 x 128 on eight wavefronts of 64 x 32; both operands go through LDS, 32 contraction indices at a time, those
+// of the next two stages on their way in registers.
+constexpr int kTile = 4, kStagePairs = 2 * kTile * 2;        // bands of a tile's side; pairs of a stage
+constexpr int kTileThreads = 512;
+template <int MODE, typename G, typename E>
+__global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* ws) {
+  __shared__ __attribute__((aligned(16))) _Float16 staged[2][kStagePairs * kPair];
+  const At at = find(c);
+  if (at.matrix >= at.l.count) return;
+  const Place p = place(at.l.mb, at.l.nb);
+  _Float16* base = halves_of(ws, at, p);
+  const int side = (p.mb + kTile - 1) / kTile;
+  int unit = at.unit, ti, tj;
+  const Product o = product_of<MODE>(c, at, p, base, unit, side);
+  if (MODE < kApply) {
+    triangle(side, unit, ti, tj);
+  } else {
+    const int jt = (o.jbands + kTile - 1) / kTile;
+    ti = unit / jt;
+    tj = unit - ti * jt;
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wi = wave >> 2, wj = wave & 3;
+  // this wavefront brings band `wave` of the tile's eight (four of each operand); a band beyond the edge: the last one
+  // again, its results are not stored
+  const _Float16* from = (wave < 4 ? o.left + (int64_t)min(ti * kTile + wave, o.ibands - 1) * o.inner * kPair
+                                   : o.right + (int64_t)min(tj * kTile + wave - 4, o.jbands - 1) * o.inner * kPair) + lane * 8;
+  struct Way { f16x8 v[4]; } way[2];
+  const int stages = o.inner / 2;
+  // (without conditions, so that a wait for one stage's loads leaves those of the next in flight: behind the last stage
+  // it is read again)
+  const auto fetch = [&](Way& w, int stage) {
+    const _Float16* p = from + (int64_t)min(stage, stages - 1) * 2 * kPair;
 #pragma unroll
-  for (int bi = 0; bi < 2; ++bi)
+    for (int i = 0; i < 4; ++i) w.v[i] = *(const f16x8*)(p + i * (kPair / 2));
+  };
+  const auto land = [&](const Way& w, int half) {
 #pragma unroll
-    for (int bj = 0; bj < 2; ++bj) {
-      const int ib = i0 + bi, jb = j0 + bj;
-      if (ib >= ibands || jb >= jbands) continue;
-      f32x16 v = acc[bi][bj];
-      if (MODE == kGram) {
-        v = v * (1.0f / u.x) * (u.a / u.x);
-      } else if (MODE == kPoly) {
-        const f32x16 a = get_turned(base + p.a, jb, ib, p.mb);
-        v = v * (1.0f / u.a) * (k2 * (u.b / u.a)) + a * (k1 * (u.b / u.a));
-      } else {
-        const f32x16 x = turned ? get_turned(base + p.x, jb, ib, p.nb) : get_turned(xt, jb, ib, p.mb);
-        v = v * (1.0f / u.b) * (next / u.x) + x * (k0 * (next / u.x));
-      }
-      if (MODE == kGram || MODE == kPoly) {
-        _Float16* to = base + (MODE == kGram ? p.a : p.b);
-        put_turned(to, jb, ib, p.mb, v);
-        if (ti != tj) put(to, ib, jb, p.mb, v, scratch[wave]);
-      } else if (MODE == kApply) {
-        put_turned(base + p.xt[~step & 1], jb, ib, p.mb, v);
-        put(base + p.x, ib, jb, p.nb, v, scratch[wave]);
-      } else {
-        const int j = jb * 32 + (lane & 31);
-        const float lr = c.hparams ? c.hparams[3 * at.matrix] : 0.0f, wd = c.hparams ? c.hparams[3 * at.matrix + 2] : 0.0f;
+    for (int i = 0; i < 4; ++i) *(f16x8*)&staged[half][wave * 2 * kPair + i * (kPair / 2) + lane * 8] = w.v[i];
+  };
+  Acc acc[2] = {};
+  const auto multiply = [&](int half) {
+    const _Float16* here = staged[half] + lane * 8;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const int r = ib * 32 + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3);
-          if (r >= l.rows || j >= l.cols) continue;
-          if (c.hparams) {
-            float* to = l.weight + at.matrix * l.w_matrix + r * l.w_row + j;
-            *to = fmaf(-lr * l.scale, v[k], *to * fmaf(-lr, wd, 1.0f));
-          } else {
-            ((G*)l.out)[at.matrix * l.out_matrix + r * l.out_row + j] = (G)v[k];
-          }
+    for (int k = 0; k < 2; ++k) {
+      const Pair y = load_pair(here + ((kTile + wj) * 2 + k) * kPair);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) acc[b].add(load_pair(here + ((2 * wi + b) * 2 + k) * kPair), y);
+    }
+  };
+  fetch(way[0], 0);
+  fetch(way[1], 1);
+  const StepFactors& step = head_of(ws, at).step[c.step];
+  const Factors f = factors_of<MODE>(step, o.q_task), fq = step.q;
+  const int jb = tj * kTile + wj;
+  Quad old[2][4] = {};
+  f32x4 weights[2][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int ib = ti * kTile + 2 * wi + b;
+    const int64_t place_to = turned_at(min(jb, o.jbands - 1), min(ib, o.ibands - 1), p.mb);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (MODE == kPoly || MODE == kMix || MODE == kNext) old[b][q] = get_turned(o.old + place_to + turned(q));
+      weights[b][q] = read_weights<MODE>(ends, at, ib, jb, q);
+    }
+  }
+  land(way[0], 0);
+  fetch(way[0], 2);
+  __syncthreads();
+  for (int g = 0; g + 1 < stages; g += 2) {
+    multiply(0);
+    land(way[1], 1);
+    fetch(way[1], g + 3);
+    __syncthreads();
+    multiply(1);
+    land(way[0], 0);
+    fetch(way[0], g + 4);
+    __syncthreads();
+  }
+  if (stages & 1) multiply(0);
+  __syncthreads();
+  unsigned* scratch = (unsigned*)staged + wave * 32 * kStride;
+  const bool mirrored = MODE == kApply || (MODE < kApply && ti != tj);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int ib = ti * kTile + 2 * wi + b;
+    if (ib >= o.ibands || jb >= o.jbands) continue;
+    f32x4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 before = value(old[b][q]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[q][r] = (acc[b].large[4 * q + r] + acc[b].small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
+    }
+    if constexpr (MODE == kLast) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) write_result<G>(ends, at, ib, jb, q, weights[b][q], v[q]);
+    } else {
+      const int64_t place_to = turned_at(jb, ib, p.mb), mirror_to = pair_at(ib, 2 * jb, MODE == kApply ? p.nb : p.mb);
+      const auto write = [&](_Float16* to, _Float16* mirror) {
+        Quad h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          h[q] = split(v[q]);
+          put_turned(to + place_to + turned(q), h[q]);
         }
+        if (!mirrored) return;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) stage(scratch, q, h[q]);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) put(mirror + mirror_to + half * kPair, scratch, half);
+      };
+      write(o.to, o.mirror);
+      if (MODE == kPoly && c.first_step) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = first_q(fq, ib, jb, q, v[q]);
+        write(base + p.q[0], base + p.q[0]);
       }
     }
+  }
+}
+
+// All m x m products of a segment for m <= 64: a matrix per workgroup, a block per wavefront, everything in LDS.
+__global__ void __launch_bounds__(kThreads) k_small(Args c, int steps, char* ws) {
+  constexpr int kArray = kSmall * kSmall * 2 * kPair;
+  __shared__ __attribute__((aligned(16))) _Float16 sA[kArray], sB[kArray], sT[kArray], sQ[kArray];
+  const At at = find(c);
+  if (at.matrix >= at.l.count) return;
+  const Place p = place(at.l.mb, at.l.nb);
+  _Float16* base = halves_of(ws, at, p);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ib = wave >> 1, jb = wave & 1, inner = 2 * p.mb, words = p.mb * p.mb * 2 * kPair / 8;
+  const bool on = ib < p.mb && jb < p.mb;
+  const int place_to = (int)turned_at(jb, ib, p.mb);
+  for (int i = threadIdx.x; i < words; i += kThreads) ((f16x8*)sA)[i] = ((const f16x8*)(base + p.a))[i];
+  const StepFactors* step = head_of(ws, at).step + c.step;
+  __syncthreads();
+  // registers of f * left * right + g * right (kPoly: old = left = right)
+  const auto multiply = [&](const _Float16* left, const _Float16* right, const Factors& f, f32x4 (&v)[4]) {
+    Acc acc = {};
+    for (int k = 0; k < inner; ++k) acc.add(load_pair(left + (ib * inner + k) * kPair + lane * 8), load_pair(right + (jb * inner + k) * kPair + lane * 8));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 before = value(get_turned(right + place_to + turned(q)));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[q][r] = (acc.large[4 * q + r] + acc.small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
+    }
+  };
+  const auto write = [&](_Float16* to, const f32x4 (&v)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put_turned(to + place_to + turned(q), split(v[q]));
+  };
+  for (int k = 0; k < steps; ++k) {
+    const StepFactors f = step[k];
+    f32x4 v[4];
+    if (on) {
+      multiply(sA, sA, f.poly, v);
+      write(sB, v);
+      if (k == 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = first_q(f.q, ib, jb, q, v[q]);
+        write(sQ, v);
+      }
+    }
+    __syncthreads();
+    if (k > 0) {
+      if (on) multiply(sB, sQ, f.q, v);
+      __syncthreads();
+      if (on) write(sQ, v);
+    }
+    if (k + 1 < steps) {
+      if (on) {
+        multiply(sB, sA, f.t, v);
+        write(sT, v);
+      }
+      __syncthreads();
+      if (on) {
+        multiply(sB, sT, f.next, v);
+        write(sA, v);
+      }
+    }
+    __syncthreads();
+  }
+  _Float16* to = base + p.q[c.done_parity];
+  for (int i = threadIdx.x; i < words; i += kThreads) ((f16x8*)to)[i] = ((const f16x8*)sQ)[i];
 }
 
 // no steps: X itself
 template <typename G>
-__global__ void __launch_bounds__(kThreads) k_no_steps(NsCall c, Work w, char* ws) {
-  __shared__ double red[kThreads];
-  const At at = find(w);
-  const NsLayer& l = c.layer[at.layer];
-  const float inv = (float)(1.0 / (norm_of(sums_of(ws, w, at), parts(l.rows, l.cols), red) + (double)c.eps));
-  const int64_t e = part_elements(l.rows, l.cols), n = (int64_t)l.rows * l.cols;
-  const int64_t lo = at.unit * e, hi = lo + e < n ? lo + e : n;
-  const float* hp = c.hparams ? c.hparams + 3 * at.matrix : nullptr;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const int r = (int)(i / l.cols), k = (int)(i % l.cols);
+__global__ void __launch_bounds__(kThreads) k_no_steps(Args c, Ends ends, char* ws) {
+  __shared__ double red[4];
+  const At at = find(c);
+  const EndArg l = ends.layer[at.layer];
+  if (at.matrix >= at.l.count) return;
+  const float inv = (float)(1.0 / (norm_of(head_of(ws, at).sums, parts(l.rows, l.cols), red) + (double)ends.eps));
+  const int e = part_elements(l.rows, l.cols), n = l.rows * l.cols;
+  const int lo = at.unit * e, hi = min(lo + e, n);
+  const float* hp = ends.hparams ? ends.hparams + 3 * at.matrix : nullptr;
+  for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
+    const int r = i / l.cols, k = i - r * l.cols;
     const float g = (float)((const G*)l.g)[at.matrix * l.g_matrix + r * l.g_row + k];
     if (hp) {
-      const float m = l.momentum[at.matrix * l.m_matrix + r * l.m_row + k], u = c.nesterov ? fmaf(hp[1], m, g) : m;
-      float* to = l.weight + at.matrix * l.w_matrix + r * l.w_row + k;
+      const float m = l.m[at.matrix * l.m_matrix + r * l.m_row + k], u = ends.nesterov ? fmaf(hp[1], m, g) : m;
+      float* to = (float*)l.out + at.matrix * l.out_matrix + r * l.out_row + k;
       *to = fmaf(-hp[0] * l.scale, u * inv, *to * fmaf(-hp[0], hp[2], 1.0f));
     } else {
       ((G*)l.out)[at.matrix * l.out_matrix + r * l.out_row + k] = (G)(g * inv);
@@ -362,42 +730,96 @@ __global__ void __launch_bounds__(kThreads) k_no_steps(NsCall c, Work w, char* w
   }
 }
 
-template <typename F> bool work_of(const NsCall& c, F per, Work& w, int64_t& blocks) {
+// ---- launches
+
+// Fills in a launch's workgroups, `per(layer, place)` for each matrix; returns their number.
+template <typename F> int lay_out(const NsCall& c, Args& a, F per) {
   int64_t off = 0;
-  blocks = 0;
-  for (int k = 0; k < c.n_layers; ++k) {
+  int blocks = 0;
+  for (int k = 0; k < POP_MUON_MAX_LAYERS; ++k) {
+    a.first[k] = k < c.n_layers ? blocks : 0x7fffffff;
+    a.layer[k] = LayerArg{};
+    if (k >= c.n_layers) continue;
     const NsLayer& l = c.layer[k];
-    w.first[k] = (int)blocks;
-    w.per[k] = per(l);
-    w.ws[k] = off;
-    blocks += (int64_t)l.count * w.per[k];
-    if (blocks >= (1ll << 24)) return false;      // 2^32 work items
+    const Place p = place_of(l.rows, l.cols);
+    a.layer[k] = {per(l, p), l.count, p.mb, p.nb, off, l.rows > l.cols};
+    blocks += ((l.count < 8 ? l.count : (l.count + 7) / 8 * 8) * a.layer[k].per + 7) / 8 * 8;
     off += ns_workspace_bytes(l.count, l.rows, l.cols);
   }
-  for (int k = c.n_layers; k <= POP_MUON_MAX_LAYERS; ++k) w.first[k] = (int)blocks;
-  return true;
+  // a layer without workgroups starts where the next one does, and is passed over
+  return blocks;
 }
 
-template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t s) {
+Args args_of(int step, int first, int last, int xt) {
+  Args a = {};
+  a.step = step;
+  a.first_step = step == first; a.last_step = step == last;
+  a.parity = (step - first) & 1; a.done_parity = (last - first) & 1;
+  a.xt = xt;
+  return a;
+}
+
+constexpr int kTilesFrom = 128;             // tiles of 128 x 128 in a launch from which they are ahead of single blocks
+
+template <int MODE, typename G, typename E, typename N>
+void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
   const auto up = [](int v) { return (v + kTile - 1) / kTile; };
-  Work sums, start, square, full;
-  int64_t n_sums, n_start, n_square, n_full;
-  if (!work_of(c, [](const NsLayer& l) { return parts(l.rows, l.cols); }, sums, n_sums) ||
-      !work_of(c, [](const NsLayer& l) { const Place p = place(l.rows, l.cols); return (p.mb * p.nb + 3) / 4; }, start, n_start) ||
-      !work_of(c, [&](const NsLayer& l) { const int t = up(place(l.rows, l.cols).mb); return t * (t + 1) / 2; }, square, n_square) ||
-      !work_of(c, [&](const NsLayer& l) { const Place p = place(l.rows, l.cols); return up(p.mb) * up(p.nb); }, full, n_full))
-    return hipErrorInvalidConfiguration;
-  k_norms<G><<<dim3(n_sums), kThreads, 0, s>>>(c, sums, ws);
+  const int big = lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, up(p.mb), up(p.nb)); });
+  if (big == 0) return;
+  if (big >= kTilesFrom) {
+    k_tile<MODE, G><<<dim3(big), kTileThreads, 0, stream>>>(a, ends, ws);
+  } else {
+    const int blocks = lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, p.mb, p.nb); });
+    k_block<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+  }
+}
+
+template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stream) {
+  Ends ends = {};
+  ends.hparams = c.hparams;
+  ends.eps = c.eps;
+  ends.nesterov = c.nesterov;
+  for (int k = 0; k < c.n_layers; ++k) {
+    const NsLayer& l = c.layer[k];
+    if (c.hparams) ends.layer[k] = {l.g, l.g_matrix, l.g_row, l.momentum, l.m_matrix, l.m_row, l.weight, l.w_matrix, l.w_row, l.rows, l.cols, l.scale, 0};
+    else ends.layer[k] = {l.g, l.g_matrix, l.g_row, nullptr, 0, 0, l.out, l.out_matrix, l.out_row, l.rows, l.cols, l.scale, 0};
+  }
+  Args a = {};
+  Bounds bounds;
+  bounds.steps = c.steps;
+  bounds.most = c.most;
+  for (int k = 0; k < POP_NS_MAX_STEPS; ++k) {
+    for (int i = 0; i < 3; ++i) bounds.coef[k][i] = c.coef[k][i];
+    bounds.gain[k] = c.gain[k];
+    bounds.q_most[k] = c.q_most[k];
+  }
+  bounds.gain[POP_NS_MAX_STEPS] = c.gain[POP_NS_MAX_STEPS];
+  int blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return parts(l.rows, l.cols); });
+  k_norms<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
   if (c.steps == 0) {
-    k_no_steps<G><<<dim3(n_sums), kThreads, 0, s>>>(c, sums, ws);
+    k_no_steps<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
     return hipGetLastError();
   }
-  k_start<G><<<dim3(n_start), kThreads, 0, s>>>(c, start, ws);
-  for (int i = 0; i < c.steps; ++i) {
-    k_product<kGram, G><<<dim3(n_square), kThreads, 0, s>>>(c, square, ws, i);
-    k_product<kPoly, G><<<dim3(n_square), kThreads, 0, s>>>(c, square, ws, i);
-    if (i + 1 < c.steps) k_product<kApply, G><<<dim3(n_full), kThreads, 0, s>>>(c, full, ws, i);
-    else k_product<kLast, G><<<dim3(n_full), kThreads, 0, s>>>(c, full, ws, i);
+  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return (p.mb * p.nb + 3) / 4; });
+  k_start<G><<<dim3(blocks), kThreads, 0, stream>>>(a, bounds, ends, ws);
+  const NoEnds none;
+  const auto square = [](const Place& p, int m, int) { return p.mb <= kSmall ? 0 : tiles(m); };
+  for (int first = 0, xt = 0; first < c.steps; first += kNsSegment, xt ^= 1) {
+    const int last = (first + kNsSegment < c.steps ? first + kNsSegment : c.steps) - 1;
+    launch_product<kGram, float>(c, args_of(first, first, last, xt), none, ws, stream, [](const Place&, int m, int) { return tiles(m); });
+    Args small = args_of(first, first, last, xt);
+    blocks = lay_out(c, small, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 1 : 0; });
+    if (blocks) k_small<<<dim3(blocks), kThreads, 0, stream>>>(small, last - first + 1, ws);
+    for (int k = first; k <= last; ++k) {
+      const Args s = args_of(k, first, last, xt);
+      launch_product<kPoly, float>(c, s, none, ws, stream, square);
+      launch_product<kMix, float>(c, s, none, ws, stream, [&](const Place& p, int m, int n) { return square(p, m, n) * ((k > first) + (k < last)); });
+      if (k < last) launch_product<kNext, float>(c, s, none, ws, stream, square);
+    }
+    const Args s = args_of(last, first, last, xt);
+    const auto full = [](const Place&, int m, int n) { return m * n; };
+    if (last + 1 < c.steps) launch_product<kApply, float>(c, s, none, ws, stream, full);
+    else launch_product<kLast, G>(c, s, ends, ws, stream, full);
   }
   return hipGetLastError();
 }
@@ -406,7 +828,7 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t s) {
 }  // namespace
 
 int64_t ns_workspace_bytes(int count, int rows, int cols) {
-  return ns::sum_bytes(count) + count * ns::place(rows, cols).size * 2;     // whole 2 KB blocks
+  return ns::head_bytes(count) + count * ns::place_of(rows, cols).size * 2;     // whole 2 KB blocks
 }
 
 hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s) {

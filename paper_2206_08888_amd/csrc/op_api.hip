@@ -65,10 +65,10 @@ int check_workspace(void* p, int64_t have, int64_t need) {
   return POP_OK;
 }
 
-// NsCall::most and gain.  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
+// NsCall::most, gain and q_most.  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
 // in s^2; p(s) / s at an end or where its derivative in s^2 is 0.
 void bounds_of(const pop_ns_config& c, NsCall& n) {
-  double top = 1.0, gain = 1.0;
+  double top = 1.0, gain = 1.0, in_segment = 1.0;
   n.most = 1.0f;
   for (int k = 0; k < c.steps; ++k) {
     n.gain[k] = (float)fmin(gain, 1e30);
@@ -82,6 +82,8 @@ void bounds_of(const pop_ns_config& c, NsCall& n) {
     if (k2 != 0.0 && -k1 / (2 * k2) > 0.0 && -k1 / (2 * k2) < end) most = fmax(most, ratio(-k1 / (2 * k2)));
     top = next;
     gain *= most;
+    in_segment = (k % kNsSegment == 0 ? 1.0 : in_segment) * most;
+    n.q_most[k] = (float)fmin(in_segment, 1e30);
     n.most = (float)fmax(n.most, top);
     if (!(n.most <= kMostSingular)) return;
   }
@@ -109,8 +111,8 @@ int check_ns(const pop_ns_config* c, int32_t dtype, NsCall& n) {
 int check_shape(int64_t count, int64_t rows, int64_t cols) {
   if (count < 1 || rows < 1 || cols < 1) return fail_thread(POP_EINVAL, "a matrix count, rows or cols is not positive");
   if (rows > kNsMaxSide || cols > kNsMaxSide) return fail_thread(POP_EUNSUPPORTED, "rows and cols must be at most %d", kNsMaxSide);
-  // workgroups take at least a 32 x 32 block; a launch has fewer than 2^24 of them
-  if (count * ((rows + 31) / 32) * ((cols + 31) / 32) >= 1 << 20) return fail_thread(POP_EUNSUPPORTED, "more than 2^20 blocks of 32 x 32 in %lld matrices", (long long)count);
+  // a launch has at most two workgroups per 32 x 32 block of each of 8 layers; its work items stay below 2^32
+  if ((count + 7) * ((rows + 31) / 32) * ((cols + 31) / 32) >= 1 << 20) return fail_thread(POP_EUNSUPPORTED, "more than 2^20 blocks of 32 x 32 in %lld matrices", (long long)count);
   return POP_OK;
 }
 
