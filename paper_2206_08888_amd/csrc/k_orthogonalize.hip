@@ -191,17 +191,26 @@ __global__ void __launch_bounds__(kThreads) k_norms(Args c, Ends ends, char* ws)
   // rows without gaps are one run of elements
   const bool flat = l.g_row == l.cols && (!m || l.m_row == l.cols);
   double sum = 0.0;
-#pragma unroll 8
-  for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
-    const int r = flat ? 0 : i / l.cols, k = flat ? i : i - r * l.cols;
-    float u = (float)g[r * l.g_row + k];
-    if (m) {
-      float* to = m + r * l.m_row + k;
-      const float v = fmaf(mu, *to, u);
-      *to = v;
-      u = ends.nesterov ? fmaf(mu, v, u) : v;
+  // eight elements at a time: all loads ahead of the stores, which the compiler could not move them past
+  for (int i0 = lo + (int)threadIdx.x; i0 < hi; i0 += 8 * kThreads) {
+    float u[8], v[8];
+    int64_t to[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * kThreads, r = flat ? 0 : i / l.cols, k = flat ? i : i - r * l.cols;
+      to[j] = r * l.m_row + k;
+      u[j] = i < hi ? (float)g[r * l.g_row + k] : 0.0f;
+      v[j] = m && i < hi ? m[to[j]] : 0.0f;
     }
-    sum += (double)u * u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (m) {
+        v[j] = fmaf(mu, v[j], u[j]);
+        if (i0 + j * kThreads < hi) m[to[j]] = v[j];
+        u[j] = ends.nesterov ? fmaf(mu, v[j], u[j]) : v[j];
+      }
+      sum += (double)u[j] * u[j];
+    }
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) head_of(ws, at).sums[at.unit] = sum;
@@ -451,6 +460,24 @@ template <typename G> __device__ inline void write_result(const Ends& ends, cons
   }
 }
 
+// A wavefront's block of results in both orders (mirror: or NULL).
+__device__ inline void write_block(const f32x4 (&v)[4], _Float16* to, _Float16* mirror, unsigned* scratch) {
+  Quad h[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    h[q] = split(v[q]);
+    put_turned(to + turned(q), h[q]);
+  }
+  if (!mirror) return;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) stage(scratch, q, h[q]);
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int half = 0; half < 2; ++half) put(mirror + half * kPair, scratch, half);
+  __builtin_amdgcn_wave_barrier();
+}
+
 // One 32 x 32 block per workgroup; the wavefronts take a quarter of the contraction each, then a quarter of the block.
 template <int MODE, typename G, typename E>
 __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
@@ -518,6 +545,79 @@ __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
   }
 }
 
+// kMix and kApply: tiles of 64 x 64, a block per wavefront, operands straight from the caches into registers, four blocks of the contraction
+// ahead.
+constexpr int kQuad = 2;                    // bands of a tile's side
+template <int MODE, typename G, typename E>
+__global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
+  __shared__ __attribute__((aligned(16))) unsigned all_scratch[4][32 * kStride];
+  const At at = find(c);
+  if (at.matrix >= at.l.count) return;
+  const Place p = place(at.l.mb, at.l.nb);
+  _Float16* base = halves_of(ws, at, p);
+  const int side = (p.mb + kQuad - 1) / kQuad;
+  int unit = at.unit, ti, tj;
+  const Product o = product_of<MODE>(c, at, p, base, unit, side);
+  if (MODE < kApply) {
+    triangle(side, unit, ti, tj);
+  } else {
+    const int jt = (o.jbands + kQuad - 1) / kQuad;
+    ti = unit / jt;
+    tj = unit - ti * jt;
+  }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ib = ti * kQuad + (wave >> 1), jb = tj * kQuad + (wave & 1);
+  if (ib >= o.ibands || jb >= o.jbands) return;
+  const _Float16 *lp = o.left + (int64_t)ib * o.inner * kPair + lane * 8, *rp = o.right + (int64_t)jb * o.inner * kPair + lane * 8;
+  struct Batch { Pair x[4], y[4]; } ahead[2];
+  // (behind the end the last blocks are read again, and not used: no conditions, as in k_tile)
+  const auto fetch = [&](Batch& b, int k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at_k = (int64_t)min(k + i, o.inner - 1) * kPair;
+      b.x[i] = load_pair(lp + at_k);
+      b.y[i] = load_pair(rp + at_k);
+    }
+  };
+  Acc acc = {};
+  const auto multiply = [&](const Batch& b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc.add(b.x[i], b.y[i]);
+  };
+  fetch(ahead[0], 0);
+  fetch(ahead[1], 4);
+  const StepFactors& step = head_of(ws, at).step[c.step];
+  const Factors f = factors_of<MODE>(step, o.q_task);
+  const int64_t place_to = turned_at(jb, ib, p.mb), mirror_to = pair_at(ib, 2 * jb, MODE == kApply ? p.nb : p.mb);
+  Quad old[4] = {};
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (MODE == kMix) old[q] = get_turned(o.old + place_to + turned(q));
+  const int whole = o.inner / 8 * 8;
+  for (int k = 0; k < whole; k += 8) {
+    multiply(ahead[0]);
+    fetch(ahead[0], k + 8);
+    multiply(ahead[1]);
+    fetch(ahead[1], k + 12);
+  }
+  if (o.inner & 4) {
+    multiply(ahead[0]);
+    ahead[0] = ahead[1];
+  }
+  if (o.inner & 2) {                          // `inner` is even
+    acc.add(ahead[0].x[0], ahead[0].y[0]);
+    acc.add(ahead[0].x[1], ahead[0].y[1]);
+  }
+  f32x4 v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const f32x4 before = value(old[q]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[q][r] = (acc.large[4 * q + r] + acc.small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
+  }
+  const bool mirrored = MODE == kApply || ti != tj;
+  write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, all_scratch[wave]);
+}
+
 // Tiles of 128 x 128 on eight wavefronts of 64 x 32; both operands go through LDS, 32 contraction indices at a time, those
 // of the next two stages on their way in registers.
 constexpr int kTile = 4, kStagePairs = 2 * kTile * 2;        // bands of a tile's side; pairs of a stage
@@ -572,18 +672,6 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
   const StepFactors& step = head_of(ws, at).step[c.step];
   const Factors f = factors_of<MODE>(step, o.q_task), fq = step.q;
   const int jb = tj * kTile + wj;
-  Quad old[2][4] = {};
-  f32x4 weights[2][4];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int ib = ti * kTile + 2 * wi + b;
-    const int64_t place_to = turned_at(min(jb, o.jbands - 1), min(ib, o.ibands - 1), p.mb);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (MODE == kPoly || MODE == kMix || MODE == kNext) old[b][q] = get_turned(o.old + place_to + turned(q));
-      weights[b][q] = read_weights<MODE>(ends, at, ib, jb, q);
-    }
-  }
   land(way[0], 0);
   fetch(way[0], 2);
   __syncthreads();
@@ -598,6 +686,18 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
     __syncthreads();
   }
   if (stages & 1) multiply(0);
+  Quad old[2][4] = {};
+  f32x4 weights[2][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int ib = ti * kTile + 2 * wi + b;
+    const int64_t place_to = turned_at(min(jb, o.jbands - 1), min(ib, o.ibands - 1), p.mb);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (MODE == kPoly || MODE == kMix || MODE == kNext) old[b][q] = get_turned(o.old + place_to + turned(q));
+      weights[b][q] = read_weights<MODE>(ends, at, ib, jb, q);
+    }
+  }
   __syncthreads();
   unsigned* scratch = (unsigned*)staged + wave * 32 * kStride;
   const bool mirrored = MODE == kApply || (MODE < kApply && ti != tj);
@@ -617,26 +717,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
       for (int q = 0; q < 4; ++q) write_result<G>(ends, at, ib, jb, q, weights[b][q], v[q]);
     } else {
       const int64_t place_to = turned_at(jb, ib, p.mb), mirror_to = pair_at(ib, 2 * jb, MODE == kApply ? p.nb : p.mb);
-      const auto write = [&](_Float16* to, _Float16* mirror) {
-        Quad h[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          h[q] = split(v[q]);
-          put_turned(to + place_to + turned(q), h[q]);
-        }
-        if (!mirrored) return;
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) stage(scratch, q, h[q]);
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int half = 0; half < 2; ++half) put(mirror + mirror_to + half * kPair, scratch, half);
-      };
-      write(o.to, o.mirror);
+      write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, scratch);
       if (MODE == kPoly && c.first_step) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = first_q(fq, ib, jb, q, v[q]);
-        write(base + p.q[0], base + p.q[0]);
+        write_block(v, base + p.q[0] + place_to, mirrored ? base + p.q[0] + mirror_to : nullptr, scratch);
       }
     }
   }
@@ -759,19 +844,32 @@ Args args_of(int step, int first, int last, int xt) {
   return a;
 }
 
-constexpr int kTilesFrom = 128;             // tiles of 128 x 128 in a launch from which they are ahead of single blocks
+// Which kernel a product takes, by the tiles of the whole launch (us, 256 x 256 matrices: k_block / k_quad / k_tile).
+// 8 matrices, X X^T 4.8 / 6.0 / 9.5, X = Q X 7.7 / 7.2 / 11.2; 16: 5.9 / 6.7 / 10.0, 11.7 / 8.8 / 12.1, two products of
+// kMix 9.9 / 8.5 / 13.0; 40: 10.0 / 10.9 / 11.4, 20.6 / 16.5 / 14.3; 80: 15.8 / 18.2 / 15.0, 39.6 / 27.3 / 26.2; one of
+// 2048 x 2048: 71 / 61 / 49, 107 / 89 / 61.
+constexpr int kTilesFrom = 128, kQuadsFrom = 128;
 
 template <int MODE, typename G, typename E, typename N>
 void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
-  const auto up = [](int v) { return (v + kTile - 1) / kTile; };
-  const int big = lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, up(p.mb), up(p.nb)); });
-  if (big == 0) return;
-  if (big >= kTilesFrom) {
-    k_tile<MODE, G><<<dim3(big), kTileThreads, 0, stream>>>(a, ends, ws);
-  } else {
-    const int blocks = lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, p.mb, p.nb); });
-    k_block<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+  const auto with = [&](int side) {
+    return lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, (p.mb + side - 1) / side, (p.nb + side - 1) / side); });
+  };
+  int blocks = with(kTile);
+  if (blocks == 0) return;
+  if (blocks >= kTilesFrom) {
+    k_tile<MODE, G><<<dim3(blocks), kTileThreads, 0, stream>>>(a, ends, ws);
+    return;
   }
+  if constexpr (MODE == kMix || MODE == kApply) {
+    blocks = with(kQuad);
+    if (blocks >= kQuadsFrom && (MODE == kApply || !(a.first_step || a.last_step))) {
+      k_quad<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+      return;
+    }
+  }
+  blocks = with(1);
+  k_block<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
 }
 
 template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stream) {
