@@ -353,7 +353,7 @@ enum { POP_F32 = 0, POP_BF16 = 1, POP_F16 = 2 };   /* element types */
  *   a_t = sigmoid(g_t + bias[i, c]),   h_t = a_t * h_{t-1} + (1 - a_t) * x_t,   y_t = h_t     for 0 <= t < length
  *
  * with h_{-1} = h0 and, where reset_t is not zero, 0 in place of h_{t-1} (an episode starts at t).  Steps from a
- * sequence's length on are never read; y is 0 there and so are the gradients.  States, sums and gates are fp32
+ * sequence's length on are not used; y is 0 there and so are the gradients.  States, sums and gates are fp32
  * whatever the arrays' type; values are rounded once, when they are stored. */
 typedef struct {
   int32_t P, batch;     /* agents, sequences of each agent */

@@ -112,7 +112,7 @@ class Recurrence(_Operator):
 
     x, g and the gradients: [P, batch, T', C] of `dtype`, T' <= T, any strides with adjacent channels.  bias [P, C],
     h0, h_last, dh_last, dh0 [P, batch, C] are float32; reset [P, batch, T'] is uint8 or bool; lengths [P, batch] is
-    int32: steps from a sequence's length on are not read, their outputs are zero."""
+    int32: steps from a sequence's length on are not used, their outputs are zero."""
 
     def __init__(self, P, batch, T, C, dtype=torch.float32, device="cuda"):
         super().__init__(dtype, device)
