@@ -610,23 +610,32 @@ __global__ void __launch_bounds__(kThreads) k_bias_sum(const float* sums, float*
 
 // ---- single steps
 
-template <typename E>
+// V channels of a row per lane.
+template <typename E, int V>
 __global__ void __launch_bounds__(kThreads) k_step(RecurArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const Lane l = lane_at(a, i);
+  typedef typename Vec<E, V>::type vec;
+  typedef typename Vec<float, V>::type fvec;
+  const Lane l = lane_at(a, ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * V);
   if (!l.on) return;
   const int slot = a.slots ? a.slots[l.row] : l.b;
-  float h = 0.0f;
+  float h[V] = {};
   if (slot >= 0 && slot < a.n_slots) {
-    float* state = a.state + ((int64_t)l.p * a.n_slots + slot) * a.C + l.c;
-    const float bias = a.bias ? -kLog2e * a.bias[(int64_t)l.p * a.C + l.c] : 0.0f;
-    const Gate q = gate(fmaf((float)((const E*)a.g.data)[base(a.g, l) + l.c], -kLog2e, bias));
-    const float u = q.b * (float)((const E*)a.x.data)[base(a.x, l) + l.c];
+    fvec* state = (fvec*)(a.state + ((int64_t)l.p * a.n_slots + slot) * a.C + l.c);
+    const vec g = *(const vec*)((const E*)a.g.data + base(a.g, l) + l.c), x = *(const vec*)((const E*)a.x.data + base(a.x, l) + l.c);
     const bool r = a.reset.data && ((const uint8_t*)a.reset.data)[base(a.reset, l)] != 0;
-    h = r ? u : fmaf(q.a, *state, u);
-    *state = h;
+    const fvec before = *state;
+    fvec bias = {}, after;
+    if (a.bias) bias = *(const fvec*)(a.bias + (int64_t)l.p * a.C + l.c);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Gate q = gate(fmaf(element<V>(g, v), -kLog2e, -kLog2e * element<V>(bias, v)));
+      const float u = q.b * element<V>(x, v);
+      h[v] = r ? u : fmaf(q.a, element<V>(before, v), u);
+      if constexpr (V == 1) after = h[v]; else after[v] = h[v];
+    }
+    *state = after;
   }
-  ((E*)a.y.data)[base(a.y, l) + l.c] = (E)h;
+  store<E, V>((typename Walk<E, V>::pointer)((E*)a.y.data + base(a.y, l) + l.c), h);
 }
 
 // ---- launches
@@ -721,7 +730,12 @@ template <typename E> hipError_t backward(const RecurArgs& a, hipStream_t s) {
 }
 
 template <typename E> hipError_t step(const RecurArgs& a, hipStream_t s) {
-  k_step<E><<<blocks((int64_t)a.P * a.B * a.C), kThreads, 0, s>>>(a);
+  const int64_t n = (int64_t)a.P * a.B * a.C, e = sizeof(E);
+  const auto row = [&](const pop_sequence& q) { return (uintptr_t)q.data % (4 * e) == 0 && q.agent % 4 == 0 && q.row % 4 == 0; };
+  if (a.C % 4 == 0 && row(a.x) && row(a.g) && row(a.y) && (uintptr_t)a.state % 16 == 0 && (uintptr_t)a.bias % 16 == 0)
+    k_step<E, 4><<<blocks(n / 4), kThreads, 0, s>>>(a);
+  else
+    k_step<E, 1><<<blocks(n), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

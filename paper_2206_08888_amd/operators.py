@@ -70,7 +70,8 @@ def _dtype_code(dtype):
 
 
 class _Operator:
-    """Device and type checks, and the stream of a call."""
+    """Device and type checks, and the stream of a call.  Calls are short beside their launches, so the checks take the
+    shortest way through what is right and find out what is wrong afterwards."""
 
     def __init__(self, dtype, device):
         self.dtype, self.code = dtype, _dtype_code(dtype)
@@ -79,18 +80,23 @@ class _Operator:
             raise ValueError("device must be a cuda device, not %s" % (device,))
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = self.device.index
         self.lib = load_library()
 
     def _tensor(self, t, name, shape, dtype=None, contiguous=True):
+        dtype = dtype or self.dtype
+        try:
+            if t.shape == shape and t.dtype is dtype and t.get_device() == self.index and (not contiguous or t.is_contiguous()):
+                return t
+        except AttributeError:
+            pass
         if not isinstance(t, torch.Tensor) or t.device != self.device:
             raise ValueError("%s must be a tensor on %s" % (name, self.device))
-        if t.dtype != (dtype or self.dtype):
-            raise ValueError("%s must be of type %s, not %s" % (name, dtype or self.dtype, t.dtype))
+        if t.dtype != dtype:
+            raise ValueError("%s must be of type %s, not %s" % (name, dtype, t.dtype))
         if t.shape != shape:
             raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-        if contiguous and not t.is_contiguous():
-            raise ValueError("%s must be contiguous" % name)
-        return t
+        raise ValueError("%s must be contiguous" % name)
 
     def _pointer(self, t, name, shape, dtype=torch.float32):
         return None if t is None else self._tensor(t, name, shape, dtype).data_ptr()
@@ -100,10 +106,13 @@ class _Operator:
 
     def _call(self, fn, *args):
         """Enqueue on the current stream of this operator's device."""
-        if torch.cuda.current_device() == self.device.index:
-            return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
-        with torch.cuda.device(self.device):
-            return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        if torch.cuda.current_device() == self.index:
+            rc = fn(*args, torch.cuda.current_stream(self.index).cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(*args, torch.cuda.current_stream(self.index).cuda_stream)
+        if rc:
+            _check(rc)
 
 
 class Recurrence(_Operator):
@@ -117,35 +126,35 @@ class Recurrence(_Operator):
     def __init__(self, P, batch, T, C, dtype=torch.float32, device="cuda"):
         super().__init__(dtype, device)
         self.P, self.batch, self.T, self.C = P, batch, T, C
+        self._rows, self._channels = (P, batch, C), (P, C)
         self._cfg = pop_recurrence_config(P, batch, T, C, self.code, 0)
         self._one = pop_recurrence_config(P, batch, 1, C, self.code, 0)
+        self._one_ref = ct.byref(self._one)
         _check(self.lib.pop_recurrence_workspace_bytes(ct.byref(self._cfg)))
 
-    def _sequence(self, t, name, shape, dtype=None):
-        t = self._tensor(t, name, shape, dtype, contiguous=False)
-        s = t.stride()
-        if len(shape) == 4 and s[3] != 1 and shape[3] > 1:
+    def _sequence(self, t, name, shape):
+        """The fields of a pop_sequence of [P, batch, T, C], or [P, batch, C] for single steps."""
+        s = self._tensor(t, name, shape, contiguous=False).stride()
+        if s[-1] != 1 and self.C > 1:
             raise ValueError("%s: its channels must be adjacent" % name)
-        return pop_sequence(t.data_ptr(), s[0], s[1], s[2])
+        return t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0
+
+    def _reset(self, reset, shape):
+        if reset is None:
+            return None, 0, 0, 0
+        dtype = torch.bool if getattr(reset, "dtype", None) is torch.bool else torch.uint8
+        s = self._tensor(reset, "reset", shape, dtype, contiguous=False).stride()
+        return reset.data_ptr(), s[0], s[1], s[2] if len(s) == 3 else 0
 
     def _io(self, x, g, bias, h0, reset, lengths):
         T = x.shape[2] if x.dim() == 4 else -1
         if T < 0 or T > self.T:
             raise ValueError("x must have shape [%d, %d, up to %d, %d], not %s" % (self.P, self.batch, self.T, self.C, tuple(x.shape)))
         shape = (self.P, self.batch, T, self.C)
-        io = pop_recurrence_io()
-        io.x, io.g = self._sequence(x, "x", shape), self._sequence(g, "g", shape)
-        if reset is not None:
-            io.reset = self._reset(reset, shape[:3])
-        io.bias = self._pointer(bias, "bias", (self.P, self.C))
-        io.h0 = self._pointer(h0, "h0", (self.P, self.batch, self.C))
-        io.lengths = self._pointer(lengths, "lengths", (self.P, self.batch), torch.int32)
+        io = pop_recurrence_io(self._sequence(x, "x", shape), self._sequence(g, "g", shape), (None, 0, 0, 0), self._reset(reset, shape[:3]),
+                               self._pointer(bias, "bias", shape[::3]), self._pointer(h0, "h0", self._rows), None,
+                               self._pointer(lengths, "lengths", shape[:2], torch.int32))
         return pop_recurrence_config(self.P, self.batch, T, self.C, self.code, 0), io, shape
-
-    def _reset(self, reset, shape):
-        dtype = torch.bool if getattr(reset, "dtype", None) == torch.bool else torch.uint8
-        t = self._tensor(reset, "reset", shape, dtype, contiguous=False)
-        return pop_sequence(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2) if len(shape) == 3 else 0)
 
     def _workspace(self, cfg):
         n = _check(self.lib.pop_recurrence_workspace_bytes(ct.byref(cfg)))
@@ -154,7 +163,7 @@ class Recurrence(_Operator):
     def forward(self, x, g, bias=None, h0=None, reset=None, lengths=None, save=False):
         """(y, h_last); with save also the states that `backward` needs: (y, h_last, states)."""
         cfg, io, shape = self._io(x, g, bias, h0, reset, lengths)
-        y, h_last = self._empty(shape), self._empty((self.P, self.batch, self.C), torch.float32)
+        y, h_last = self._empty(shape), self._empty(self._rows, torch.float32)
         io.y, io.h_last = self._sequence(y, "y", shape), h_last.data_ptr()
         states = None
         if save:
@@ -170,12 +179,9 @@ class Recurrence(_Operator):
         n = _check(self.lib.pop_recurrence_states_bytes(ct.byref(cfg))) // 4
         io.states = self._pointer(states, "states", (n,))
         dx, dg = self._empty(shape), self._empty(shape)
-        dbias, dh0 = self._empty((self.P, self.C), torch.float32), self._empty((self.P, self.batch, self.C), torch.float32)
-        grads = pop_recurrence_grads()
-        grads.dy = self._sequence(dy, "dy", shape)
-        grads.dx, grads.dg = self._sequence(dx, "dx", shape), self._sequence(dg, "dg", shape)
-        grads.dh_last = self._pointer(dh_last, "dh_last", (self.P, self.batch, self.C))
-        grads.dh0, grads.dbias = dh0.data_ptr(), dbias.data_ptr()
+        dbias, dh0 = self._empty(self._channels, torch.float32), self._empty(self._rows, torch.float32)
+        grads = pop_recurrence_grads(self._sequence(dy, "dy", shape), self._sequence(dx, "dx", shape), self._sequence(dg, "dg", shape),
+                                     self._pointer(dh_last, "dh_last", self._rows), dh0.data_ptr(), dbias.data_ptr())
         ws, n = self._workspace(cfg)
         self._call(self.lib.pop_recurrence_backward, ct.byref(cfg), ct.byref(io), ct.byref(grads), ws.data_ptr(), n)
         return dx, dg, dbias, dh0
@@ -184,26 +190,18 @@ class Recurrence(_Operator):
         """One step of acting agents: x, g, y [P, batch, C]; state [P, n_slots, C] float32 is updated in place.  slots
         [P, batch] int32 names each row's state (none twice within an agent); a row whose slot is negative or not
         below n_slots is idle and gets zeros.  Without slots row b has state b."""
-        shape = (self.P, self.batch, self.C)
-        io = pop_recurrence_io()
-        y = self._empty(shape)
-        for field, t, name in (("x", x, "x"), ("g", g, "g"), ("y", y, "y")):
-            self._tensor(t, name, shape, contiguous=False)
-            s = t.stride()
-            if s[2] != 1 and self.C > 1:
-                raise ValueError("%s: its channels must be adjacent" % name)
-            setattr(io, field, pop_sequence(t.data_ptr(), s[0], s[1], 0))
-        if reset is not None:
-            io.reset = self._reset(reset, shape[:2])
-        io.bias = self._pointer(bias, "bias", (self.P, self.C))
+        shape = self._rows
         if not isinstance(state, torch.Tensor) or state.dim() != 3:
             raise ValueError("state must be a [P, n_slots, C] tensor")
         n_slots = state.shape[1]
         if slots is None and n_slots < self.batch:
             raise ValueError("state has %d rows for %d sequences and no slots are given" % (n_slots, self.batch))
-        self._call(self.lib.pop_recurrence_step, ct.byref(self._one), ct.byref(io),
-                   self._pointer(state, "state", (self.P, n_slots, self.C)), n_slots,
-                   self._pointer(slots, "slots", (self.P, self.batch), torch.int32))
+        xs, gs = self._sequence(x, "x", shape), self._sequence(g, "g", shape)
+        y = x.new_empty(shape)
+        io = pop_recurrence_io(xs, gs, (y.data_ptr(), self.batch * self.C, self.C, 0), self._reset(reset, shape[:2]),
+                               self._pointer(bias, "bias", self._channels))
+        self._call(self.lib.pop_recurrence_step, self._one_ref, ct.byref(io), self._pointer(state, "state", (self.P, n_slots, self.C)),
+                   n_slots, self._pointer(slots, "slots", shape[:2], torch.int32))
         return y
 
 
