@@ -26,7 +26,9 @@
 // of 8 halves (lane l: row l & 31, indices 8 (l >> 5) ..), the hi block in front of the lo block, 2 KB together,
 // blocks of one row band adjacent.  Both operands have the contraction index inside, so X is kept in both orders.
 #include <hip/hip_runtime.h>
+#include <type_traits>
 #include "operators.h"
+#include "pop_dev.h"
 
 namespace pop {
 namespace {
@@ -142,8 +144,9 @@ __device__ inline StepFactors factors_of(const Bounds& c, int k, float start) {
   return f;
 }
 
-// Workgroups go to the 8 XCDs in turn; from 8 matrices on all those of one matrix go to one XCD, whose L2 then reads
-// the matrix once.
+// Workgroups go to the 8 XCDs in turn: each XCD takes an eighth of a layer's units in a row, so that its L2 reads few
+// matrices, and of large ones few bands of the left operand (20 critics of 393 x 256 and
+// 256 x 256, a step: 308 us with matrices dealt out to XCDs one by one, 246 so).  matrix < 0: none left.
 struct At { int layer, matrix, unit; LayerArg l; };
 __device__ inline At find(const Args& c) {
   const int block = (int)blockIdx.x;
@@ -152,10 +155,9 @@ __device__ inline At find(const Args& c) {
 #pragma unroll
   for (int k = 1; k < POP_MUON_MAX_LAYERS; ++k) at.layer += block >= c.first[k];
   at.l = c.layer[at.layer];
-  const int i = block - c.first[at.layer], per = at.l.per, n = at.l.count < 8 ? i : i >> 3;
-  at.matrix = n / per;
-  at.unit = n - at.matrix * per;
-  if (at.l.count >= 8) at.matrix = at.matrix * 8 + (i & 7);
+  const int i = block - c.first[at.layer], per = at.l.per, units = per * at.l.count, n = (i & 7) * ((units + 7) / 8) + (i >> 3);
+  at.matrix = n < units ? n / per : -1;
+  at.unit = n % per;
   return at;
 }
 
@@ -180,9 +182,10 @@ __device__ inline double block_sum(double v, double* red) {
 template <typename G>
 __global__ void __launch_bounds__(kThreads) k_norms(Args c, Ends ends, char* ws) {
   __shared__ double red[4];
+  warm_args<576>();
   const At at = find(c);
   const EndArg l = ends.layer[at.layer];
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const int e = part_elements(l.rows, l.cols), n = l.rows * l.cols;
   const int lo = at.unit * e, hi = min(lo + e, n);
   const float mu = ends.hparams ? ends.hparams[3 * at.matrix + 1] : 0.0f;
@@ -284,9 +287,10 @@ template <typename G>
 __global__ void __launch_bounds__(kThreads) k_start(Args c, Bounds bounds, Ends ends, char* ws) {
   __shared__ double red[4];
   __shared__ __attribute__((aligned(16))) unsigned scratch[4][32 * kStride];
+  warm_args<576>();
   const At at = find(c);
   const EndArg l = ends.layer[at.layer];
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const Place p = place(at.l.mb, at.l.nb);
   const float mu = ends.hparams ? ends.hparams[3 * at.matrix + 1] : 0.0f;
   const bool turned_in = l.rows > l.cols, plain = !ends.hparams || ends.nesterov;
@@ -341,6 +345,12 @@ __global__ void __launch_bounds__(kThreads) k_start(Args c, Bounds bounds, Ends 
 
 __device__ inline f32x16 mfma(const f16x8& a, const f16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// What waits for LDS only: loads stay in flight across it.
+__device__ inline void sync_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 struct Pair { f16x8 hi, lo; };
 __device__ inline Pair load_pair(const _Float16* p) { return {*(const f16x8*)p, *(const f16x8*)(p + kPair / 2)}; }
@@ -483,8 +493,9 @@ template <int MODE, typename G, typename E>
 __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
   __shared__ float part[4][16][64];
   __shared__ __attribute__((aligned(16))) unsigned scratch[32 * kStride];
+  warm_args<sizeof(Args) + (std::is_same<E, Ends>::value ? 256 : 0)>();
   const At at = find(c);
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const Place p = place(at.l.mb, at.l.nb);
   _Float16* base = halves_of(ws, at, p);
   int unit = at.unit, ib, jb;
@@ -551,8 +562,9 @@ constexpr int kQuad = 2;                    // bands of a tile's side
 template <int MODE, typename G, typename E>
 __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
   __shared__ __attribute__((aligned(16))) unsigned all_scratch[4][32 * kStride];
+  warm_args<sizeof(Args) + (std::is_same<E, Ends>::value ? 256 : 0)>();
   const At at = find(c);
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const Place p = place(at.l.mb, at.l.nb);
   _Float16* base = halves_of(ws, at, p);
   const int side = (p.mb + kQuad - 1) / kQuad;
@@ -618,19 +630,23 @@ __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
   write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, all_scratch[wave]);
 }
 
-// Tiles of 128 x 128 on eight wavefronts of 64 x 32; both operands go through LDS, 32 contraction indices at a time, those
-// of the next two stages on their way in registers.
-constexpr int kTile = 4, kStagePairs = 2 * kTile * 2;        // bands of a tile's side; pairs of a stage
-constexpr int kTileThreads = 512;
-template <int MODE, typename G, typename E>
+// Tiles of 128 x 64 BJ, 64 x 32 BJ per wavefront, 32 contraction indices at a time.  The right operand goes through LDS, the
+// left one, which two wavefronts share, straight into registers.  The next stage is on its way in registers.  With 2048 x
+// 2048 matrices 128 x 128 tiles run at 840 TFLOP/s of fp16 products, prologue and epilogue included, where a large fp16
+// product of the library reaches 1130.
+constexpr int kTile = 4, kTileThreads = 256;
+template <int MODE, typename G, typename E, int BJ>
 __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* ws) {
-  __shared__ __attribute__((aligned(16))) _Float16 staged[2][kStagePairs * kPair];
+  __shared__ __attribute__((aligned(16))) _Float16 staged[2][2 * BJ * 2 * kPair];
+  __shared__ __attribute__((aligned(16))) unsigned all_scratch[4][32 * kStride];
+  warm_args<sizeof(Args) + (std::is_same<E, Ends>::value ? 256 : 0)>();
   const At at = find(c);
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const Place p = place(at.l.mb, at.l.nb);
   _Float16* base = halves_of(ws, at, p);
   const int side = (p.mb + kTile - 1) / kTile;
-  int unit = at.unit, ti, tj;
+  int unit = BJ == 2 ? at.unit : at.unit >> 1, ti, tj;         // a tile of 128 x 128, and which half of it
+  const int half_of = BJ == 2 ? 0 : at.unit & 1;
   const Product o = product_of<MODE>(c, at, p, base, unit, side);
   if (MODE < kApply) {
     triangle(side, unit, ti, tj);
@@ -639,100 +655,111 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
     ti = unit / jt;
     tj = unit - ti * jt;
   }
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wi = wave >> 2, wj = wave & 3;
-  // this wavefront brings band `wave` of the tile's eight (four of each operand); a band beyond the edge: the last one
-  // again, its results are not stored
-  const _Float16* from = (wave < 4 ? o.left + (int64_t)min(ti * kTile + wave, o.ibands - 1) * o.inner * kPair
-                                   : o.right + (int64_t)min(tj * kTile + wave - 4, o.jbands - 1) * o.inner * kPair) + lane * 8;
-  struct Way { f16x8 v[4]; } way[2];
-  const int stages = o.inner / 2;
-  // (without conditions, so that a wait for one stage's loads leaves those of the next in flight: behind the last stage
-  // it is read again)
-  const auto fetch = [&](Way& w, int stage) {
-    const _Float16* p = from + (int64_t)min(stage, stages - 1) * 2 * kPair;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, wi = wave >> 1, wj = wave & 1;
+  const int ib0 = ti * kTile + 2 * wi, j_first = tj * kTile + 2 * half_of, jb0 = j_first + BJ * wj, stages = o.inner / 2;
+  // (a band beyond the edge: the last one again, its results are not stored; behind the last stage it is read again:
+  // without conditions a wait for one stage's loads leaves those of the next in flight)
+  const _Float16* lp[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w.v[i] = *(const f16x8*)(p + i * (kPair / 2));
-  };
-  const auto land = [&](const Way& w, int half) {
+  for (int b = 0; b < 2; ++b) lp[b] = o.left + (int64_t)min(ib0 + b, o.ibands - 1) * o.inner * kPair + lane * 8;
+  if (j_first >= o.jbands) return;
+  // this wavefront brings one of the right bands, or with two of them a half of one
+  const _Float16* rp = o.right + (int64_t)min(j_first + (BJ == 2 ? wave : wave >> 1), o.jbands - 1) * o.inner * kPair +
+                       (BJ == 2 ? 0 : (wave & 1) * kPair) + lane * 8;
+  struct Left { Pair v[2][2]; } left[2];
+  struct Way { f16x8 v[2 * BJ]; } way;
+  const auto fetch_left = [&](Left& l, int stage) {
+    const int64_t off = (int64_t)min(stage, stages - 1) * 2 * kPair;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *(f16x8*)&staged[half][wave * 2 * kPair + i * (kPair / 2) + lane * 8] = w.v[i];
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) l.v[b][k] = load_pair(lp[b] + off + k * kPair);
   };
-  Acc acc[2] = {};
-  const auto multiply = [&](int half) {
+  const auto fetch_right = [&](int stage) {
+    const _Float16* from = rp + (int64_t)min(stage, stages - 1) * 2 * kPair;
+#pragma unroll
+    for (int i = 0; i < 2 * BJ; ++i) way.v[i] = *(const f16x8*)(from + i * (kPair / 2));
+  };
+  const auto land = [&](int half) {
+#pragma unroll
+    for (int i = 0; i < 2 * BJ; ++i) *(f16x8*)&staged[half][wave * BJ * kPair + i * (kPair / 2) + lane * 8] = way.v[i];
+  };
+  Acc acc[2][BJ] = {};
+  const auto multiply = [&](int half, const Left& l) {
     const _Float16* here = staged[half] + lane * 8;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const Pair y = load_pair(here + ((kTile + wj) * 2 + k) * kPair);
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) acc[b].add(load_pair(here + ((2 * wi + b) * 2 + k) * kPair), y);
-    }
+      for (int j = 0; j < BJ; ++j) {
+        const Pair y = load_pair(here + ((BJ * wj + j) * 2 + k) * kPair);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[b][j].add(l.v[b][k], y);
+      }
   };
-  fetch(way[0], 0);
-  fetch(way[1], 1);
+  fetch_right(0);
+  fetch_left(left[0], 0);
+  land(0);
+  fetch_right(1);
   const StepFactors& step = head_of(ws, at).step[c.step];
   const Factors f = factors_of<MODE>(step, o.q_task), fq = step.q;
-  const int jb = tj * kTile + wj;
-  land(way[0], 0);
-  fetch(way[0], 2);
-  __syncthreads();
+  sync_lds();
+  // a stage: its right operand is in LDS half `half`, its left one in `now`; the next ones on their way
+  const auto stage_of = [&](int g, int half, const Left& now, Left& next) {
+    fetch_left(next, g + 1);
+    multiply(half, now);
+    land(half ^ 1);
+    fetch_right(g + 2);
+    sync_lds();
+  };
   for (int g = 0; g + 1 < stages; g += 2) {
-    multiply(0);
-    land(way[1], 1);
-    fetch(way[1], g + 3);
-    __syncthreads();
-    multiply(1);
-    land(way[0], 0);
-    fetch(way[0], g + 4);
-    __syncthreads();
+    stage_of(g, 0, left[0], left[1]);
+    stage_of(g + 1, 1, left[1], left[0]);
   }
-  if (stages & 1) multiply(0);
-  Quad old[2][4] = {};
-  f32x4 weights[2][4];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int ib = ti * kTile + 2 * wi + b;
-    const int64_t place_to = turned_at(min(jb, o.jbands - 1), min(ib, o.ibands - 1), p.mb);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (MODE == kPoly || MODE == kMix || MODE == kNext) old[b][q] = get_turned(o.old + place_to + turned(q));
-      weights[b][q] = read_weights<MODE>(ends, at, ib, jb, q);
-    }
-  }
-  __syncthreads();
-  unsigned* scratch = (unsigned*)staged + wave * 32 * kStride;
+  if (stages & 1) multiply(0, left[0]);
+  unsigned* scratch = all_scratch[wave];
   const bool mirrored = MODE == kApply || (MODE < kApply && ti != tj);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int ib = ti * kTile + 2 * wi + b;
-    if (ib >= o.ibands || jb >= o.jbands) continue;
-    f32x4 v[4];
+  for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 before = value(old[b][q]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[q][r] = (acc[b].large[4 * q + r] + acc[b].small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
-    }
-    if constexpr (MODE == kLast) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) write_result<G>(ends, at, ib, jb, q, weights[b][q], v[q]);
-    } else {
+    for (int bj = 0; bj < BJ; ++bj) {
+      const int ib = ib0 + bi, jb = jb0 + bj;
+      if (ib >= o.ibands || jb >= o.jbands) continue;
       const int64_t place_to = turned_at(jb, ib, p.mb), mirror_to = pair_at(ib, 2 * jb, MODE == kApply ? p.nb : p.mb);
-      write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, scratch);
-      if (MODE == kPoly && c.first_step) {
+      Quad old[4] = {};
+      f32x4 v[4], weights[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = first_q(fq, ib, jb, q, v[q]);
-        write_block(v, base + p.q[0] + place_to, mirrored ? base + p.q[0] + mirror_to : nullptr, scratch);
+      for (int q = 0; q < 4; ++q) {
+        if (MODE == kPoly || MODE == kMix || MODE == kNext) old[q] = get_turned(o.old + place_to + turned(q));
+        weights[q] = read_weights<MODE>(ends, at, ib, jb, q);
+      }
+      const Acc& sum = acc[bi][bj];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 before = value(old[q]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[q][r] = (sum.large[4 * q + r] + sum.small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
+      }
+      if constexpr (MODE == kLast) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) write_result<G>(ends, at, ib, jb, q, weights[q], v[q]);
+      } else {
+        write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, scratch);
+        if (MODE == kPoly && c.first_step) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = first_q(fq, ib, jb, q, v[q]);
+          write_block(v, base + p.q[0] + place_to, mirrored ? base + p.q[0] + mirror_to : nullptr, scratch);
+        }
       }
     }
-  }
 }
 
 // All m x m products of a segment for m <= 64: a matrix per workgroup, a block per wavefront, everything in LDS.
 __global__ void __launch_bounds__(kThreads) k_small(Args c, int steps, char* ws) {
   constexpr int kArray = kSmall * kSmall * 2 * kPair;
   __shared__ __attribute__((aligned(16))) _Float16 sA[kArray], sB[kArray], sT[kArray], sQ[kArray];
+  warm_args<sizeof(Args)>();
   const At at = find(c);
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const Place p = place(at.l.mb, at.l.nb);
   _Float16* base = halves_of(ws, at, p);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ib = wave >> 1, jb = wave & 1, inner = 2 * p.mb, words = p.mb * p.mb * 2 * kPair / 8;
@@ -795,9 +822,10 @@ __global__ void __launch_bounds__(kThreads) k_small(Args c, int steps, char* ws)
 template <typename G>
 __global__ void __launch_bounds__(kThreads) k_no_steps(Args c, Ends ends, char* ws) {
   __shared__ double red[4];
+  warm_args<576>();
   const At at = find(c);
   const EndArg l = ends.layer[at.layer];
-  if (at.matrix >= at.l.count) return;
+  if (at.matrix < 0) return;
   const float inv = (float)(1.0 / (norm_of(head_of(ws, at).sums, parts(l.rows, l.cols), red) + (double)ends.eps));
   const int e = part_elements(l.rows, l.cols), n = l.rows * l.cols;
   const int lo = at.unit * e, hi = min(lo + e, n);
@@ -828,7 +856,7 @@ template <typename F> int lay_out(const NsCall& c, Args& a, F per) {
     const NsLayer& l = c.layer[k];
     const Place p = place_of(l.rows, l.cols);
     a.layer[k] = {per(l, p), l.count, p.mb, p.nb, off, l.rows > l.cols};
-    blocks += ((l.count < 8 ? l.count : (l.count + 7) / 8 * 8) * a.layer[k].per + 7) / 8 * 8;
+    blocks += (l.count * a.layer[k].per + 7) / 8 * 8;
     off += ns_workspace_bytes(l.count, l.rows, l.cols);
   }
   // a layer without workgroups starts where the next one does, and is passed over
@@ -844,31 +872,36 @@ Args args_of(int step, int first, int last, int xt) {
   return a;
 }
 
-// Which kernel a product takes, by the tiles of the whole launch (us, 256 x 256 matrices: k_block / k_quad / k_tile).
-// 8 matrices, X X^T 4.8 / 6.0 / 9.5, X = Q X 7.7 / 7.2 / 11.2; 16: 5.9 / 6.7 / 10.0, 11.7 / 8.8 / 12.1, two products of
-// kMix 9.9 / 8.5 / 13.0; 40: 10.0 / 10.9 / 11.4, 20.6 / 16.5 / 14.3; 80: 15.8 / 18.2 / 15.0, 39.6 / 27.3 / 26.2; one of
-// 2048 x 2048: 71 / 61 / 49, 107 / 89 / 61.
-constexpr int kTilesFrom = 128, kQuadsFrom = 128;
+// Which kernel a product takes, by the 128 x 128 tiles of the whole launch (us: k_tile of 128 x 128 / of 128 x 64 / k_quad
+// for kMix and kApply, else k_block).  256 x 256 matrices, X X^T of 8: 11.0 / 7.3 / 4.7, 20: 11.8 / 8.9 / 6.5, 40: 12.7 / 10.0
+// / 9.7, 80: 14.8 / 14.5 / 15.8, 160: 24.3 / 27.0 / 28.5; X = Q X of 20: 13.3 / 10.2 / 12.4, 40: 14.2 / 14.6 / 16.2, 80: 23.0 /
+// 21.5 / 27.6; four of 1024 x 4096: X X^T 108 / 113 / 120, X = Q X 127 / 150 / 223; one of 2048 x 2048: 54 / 58 / 73.
+constexpr int kTilesFrom = 256, kHalvesFrom = 128, kQuadsFrom = 128;
 
 template <int MODE, typename G, typename E, typename N>
 void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
-  const auto with = [&](int side) {
-    return lay_out(c, a, [&](const NsLayer&, const Place& p) { return count(p, (p.mb + side - 1) / side, (p.nb + side - 1) / side); });
+  const auto with = [&](int side, int halves) {
+    return lay_out(c, a, [&](const NsLayer&, const Place& p) { return halves * count(p, (p.mb + side - 1) / side, (p.nb + side - 1) / side); });
   };
-  int blocks = with(kTile);
+  int blocks = with(kTile, 1);
   if (blocks == 0) return;
   if (blocks >= kTilesFrom) {
-    k_tile<MODE, G><<<dim3(blocks), kTileThreads, 0, stream>>>(a, ends, ws);
+    k_tile<MODE, G, E, 2><<<dim3(blocks), kTileThreads, 0, stream>>>(a, ends, ws);
+    return;
+  }
+  if (blocks >= kHalvesFrom) {
+    blocks = with(kTile, 2);
+    k_tile<MODE, G, E, 1><<<dim3(blocks), kTileThreads, 0, stream>>>(a, ends, ws);
     return;
   }
   if constexpr (MODE == kMix || MODE == kApply) {
-    blocks = with(kQuad);
+    blocks = with(kQuad, 1);
     if (blocks >= kQuadsFrom && (MODE == kApply || !(a.first_step || a.last_step))) {
       k_quad<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
       return;
     }
   }
-  blocks = with(1);
+  blocks = with(1, 1);
   k_block<MODE, G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
 }
 
