@@ -63,7 +63,7 @@ __host__ __device__ inline Place place_of(int rows, int cols) {
 constexpr int kSumParts = 256;              // most partial sums of one matrix's squares
 __host__ __device__ inline int part_elements(int rows, int cols) {
   const int64_t n = (int64_t)rows * cols, a = (n + kSumParts - 1) / kSumParts;
-  return (int)(a > 8192 ? a : 8192);
+  return (int)(a > 8192 ? (a + 1023) / 1024 * 1024 : 8192);
 }
 __host__ __device__ inline int parts(int rows, int cols) {
   const int64_t e = part_elements(rows, cols);
@@ -195,24 +195,53 @@ __global__ void __launch_bounds__(kThreads) k_norms(Args c, Ends ends, char* ws)
   const bool flat = l.g_row == l.cols && (!m || l.m_row == l.cols);
   double sum = 0.0;
   // eight elements at a time: all loads ahead of the stores, which the compiler could not move them past
-  for (int i0 = lo + (int)threadIdx.x; i0 < hi; i0 += 8 * kThreads) {
-    float u[8], v[8];
-    int64_t to[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = i0 + j * kThreads, r = flat ? 0 : i / l.cols, k = flat ? i : i - r * l.cols;
-      to[j] = r * l.m_row + k;
-      u[j] = i < hi ? (float)g[r * l.g_row + k] : 0.0f;
-      v[j] = m && i < hi ? m[to[j]] : 0.0f;
-    }
+  const auto add = [&](float (&u)[8], float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (m) {
         v[j] = fmaf(mu, v[j], u[j]);
-        if (i0 + j * kThreads < hi) m[to[j]] = v[j];
         u[j] = ends.nesterov ? fmaf(mu, v[j], u[j]) : v[j];
       }
       sum += (double)u[j] * u[j];
+    }
+  };
+  if (flat && (n & 3) == 0 && (uintptr_t)g % (4 * sizeof(G)) == 0 && (uintptr_t)m % 16 == 0) {
+    typedef G g4 __attribute__((ext_vector_type(4)));
+    for (int i0 = lo + 4 * (int)threadIdx.x; i0 < hi; i0 += 8 * kThreads) {        // two runs of four
+      const int i1 = i0 + 4 * kThreads;
+      float u[8] = {}, v[8] = {};
+      const g4 a = *(const g4*)(g + i0);
+      f32x4 c = {}, d = {};
+      g4 b = {};
+      if (m) c = *(const f32x4*)(m + i0);
+      if (i1 < hi) {
+        b = *(const g4*)(g + i1);
+        if (m) d = *(const f32x4*)(m + i1);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { u[j] = (float)a[j]; u[4 + j] = (float)b[j]; v[j] = c[j]; v[4 + j] = d[j]; }
+      add(u, v);
+      if (m) {
+        *(f32x4*)(m + i0) = f32x4{v[0], v[1], v[2], v[3]};
+        if (i1 < hi) *(f32x4*)(m + i1) = f32x4{v[4], v[5], v[6], v[7]};
+      }
+    }
+  } else {
+    for (int i0 = lo + (int)threadIdx.x; i0 < hi; i0 += 8 * kThreads) {
+      float u[8], v[8];
+      int64_t to[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + j * kThreads, r = flat ? 0 : i / l.cols, k = flat ? i : i - r * l.cols;
+        to[j] = r * l.m_row + k;
+        u[j] = i < hi ? (float)g[r * l.g_row + k] : 0.0f;
+        v[j] = m && i < hi ? m[to[j]] : 0.0f;
+      }
+      add(u, v);
+      if (m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (i0 + j * kThreads < hi) m[to[j]] = v[j];
     }
   }
   sum = block_sum(sum, red);
