@@ -2,19 +2,20 @@
 //
 //   X = U / (|U| + eps);  steps times:  A = X X^T,  B = k1 A + k2 A A,  X = k0 X + B X
 //
-// with X of m x n, m <= n (matrices with more rows than columns are taken transposed).  The steps multiply X by
-// polynomials of A, which commute, so several of them are taken in the space of A: with P = k0 + B,
+// with X of m x n, m <= n (matrices with more rows than columns are taken transposed).  A step multiplies X by P = k0 + B,
+// and several of them may be taken in the space of A, where such polynomials are symmetric m x m matrices that commute
+// (half of their tiles are computed):
 //
-//   A = X X^T;  per step:  Q = P Q,  A = P A P;  then X = Q X
+//   A = X X^T;  per step of a segment:  Q = P Q,  A = P A P;  then X = Q X
 //
-// where every product is of two commuting symmetric m x m matrices, half of whose tiles are computed.  X (m x n) is
-// touched twice per segment of steps instead of twice per step.  An error of A grows by up to k0^2 per step there, where
-// a step on X starts from a fresh A: segments of kNsSegment = 3 steps (errors against 64 bits over 256 x 256, 256 x 1024,
-// 64 x 2048 gradients 7e-7, 1.0e-6, 5e-7; all five steps in one segment 9e-6, 6e-7, 4e-7, and 3e-3 for a 31 x 32 gradient
-// with one small singular value; each step on X 2.7e-7; fp32 products 1.7e-6, 2.1e-6, 1.2e-6).
+// so that X, m x n, is touched twice per segment.  An error of A grows by up to k0^2 per step inside one.  Errors against
+// 64 bits, segments of 1 / 2 / 3 steps, over those of fp32 products: 0.78 / 1.6 / 2.6 in the mean of 40 shapes, 3 / 8 / 66 at
+// most (small square matrices, one of whose singular values is small).  So results in fp32 take one step per segment,
+// and results of 16 bits, whose rounding is 2e-4 or more, three where that is less work, from n = 1.5 m on (four 1024 x
+// 4096: 877 us, with one step 1286; 256 x 256: 114, with one 102).
 //
-// All matrices of a call advance together, a launch per product.  Layers whose m is at most 64 do all products of a
-// segment that are m x m in one workgroup.
+// All matrices of a call advance together, a launch per product.  m up to 64 has a path of its own: the squares of A, Q and
+// so on fit a workgroup, and with everything in 64 bits all steps are one segment (below, k_gram64).
 //
 // Products on v_mfma_f32_32x32x16_f16 from operands in two fp16 halves, x = hi + lo with 11 bits each, held in units
 // (powers of two, Units below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
@@ -40,7 +41,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPair = 1024;                 // halves of a hi and a lo block
-constexpr int kSmall = 2;                   // bands of m up to which one workgroup does a segment's m x m products
+constexpr int kSmall = 2;                   // bands of m up to which a matrix takes the path in 64 bits
 
 // Where the arrays of one matrix lie, in halves from the start of its workspace.
 struct Place {
@@ -69,6 +70,11 @@ __host__ __device__ inline int parts(int rows, int cols) {
   const int64_t e = part_elements(rows, cols);
   return (int)(((int64_t)rows * cols + e - 1) / e);
 }
+
+// m <= 64: partial sums of X X^T over pieces of n, and Q, in squares of 16-row bands.
+constexpr int kPieces = 32;                 // most pieces
+__host__ __device__ inline int small_side(int m) { return (m + 15) / 16 * 16; }
+__host__ __device__ inline int pieces(int n) { const int c = (n + 63) / 64; return c < kPieces ? c : kPieces; }
 
 // Factors of a step's products (two of each product, as one may not be finite) and of what is added to them.
 struct Factors { float p0, p1, old; };
@@ -124,12 +130,12 @@ __device__ inline float unit_of(float most, int limit) {
   return ldexpf(1.0f, e < limit ? e : limit);
 }
 struct Bounds {                             // NsCall
-  int steps;
+  int steps, segment;
   float most, coef[POP_NS_MAX_STEPS][3], gain[POP_NS_MAX_STEPS + 1], q_most[POP_NS_MAX_STEPS];
 };
 __device__ inline float x_most(const Bounds& c, int step, float start) { return fminf(c.most, start * c.gain[step]); }
 __device__ inline StepFactors factors_of(const Bounds& c, int k, float start) {
-  const int first = k / kNsSegment * kNsSegment;
+  const int first = k / c.segment * c.segment;
   const float k0 = c.coef[k][0], k1 = c.coef[k][1], k2 = c.coef[k][2], most = x_most(c, k, start), after = x_most(c, k + 1, start), a2 = most * most;
   const float x = unit_of(most, 100), a = unit_of(a2, 60), b = unit_of(fabsf(k1) * a2 + fabsf(k2) * a2 * a2, 60), t = unit_of(most * after, 60),
               a_next = unit_of(after * after, 60), q = unit_of(c.q_most[k], 60);
@@ -782,69 +788,226 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
     }
 }
 
-// All m x m products of a segment for m <= 64: a matrix per workgroup, a block per wavefront, everything in LDS.
-__global__ void __launch_bounds__(kThreads) k_small(Args c, int steps, char* ws) {
-  constexpr int kArray = kSmall * kSmall * 2 * kPair;
-  __shared__ __attribute__((aligned(16))) _Float16 sA[kArray], sB[kArray], sT[kArray], sQ[kArray];
-  warm_args<sizeof(Args)>();
+// ---- m <= 64, in 64 bits
+
+// The 64-bit path: k_gram64 updates the momentum and sums U U^T over a piece of n, k_square64 adds the pieces up (the trace
+// is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Vector instructions: their
+// 64-bit rate is that of the matrix ones.  Errors: the rounding of the result.  Three launches: 17 x 2000 FIG1 us, 8 of 64 x
+// 2048 FIG2, bound by the latency of three launches and, for m = 64, by the 17 products of one workgroup.
+
+constexpr int kChunk = 64, kChunkStride = 65;
+// U's columns (of X) j0 .. j0 + 63 to LDS, zeros outside; `update`: with the momentum's step.
+template <typename G> __device__ inline void load_chunk(const Ends& ends, const EndArg& l, int matrix, bool update, int j0, float (*x)[kChunkStride]) {
+  const bool turned_in = l.rows > l.cols;
+  const int m = turned_in ? l.cols : l.rows, n = turned_in ? l.rows : l.cols, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float mu = ends.hparams ? ends.hparams[3 * matrix + 1] : 0.0f;
+  const G* g = (const G*)l.g + matrix * l.g_matrix;
+  float* mom = ends.hparams ? l.m + matrix * l.m_matrix : nullptr;
+  float u[16], v[16];
+  // lanes along the caller's columns, four rows at a time: rows and columns of this chunk
+  const int c0 = turned_in ? 0 : j0, r0 = turned_in ? j0 : 0, rows = turned_in ? min(n - j0, 64) : m, cols = turned_in ? m : min(n - j0, 64);
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int r = wave + 4 * k;
+    const bool in = r < rows && lane < cols;
+    u[k] = in ? (float)g[(r0 + r) * l.g_row + c0 + lane] : 0.0f;
+    v[k] = in && mom ? mom[(r0 + r) * l.m_row + c0 + lane] : 0.0f;
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int r = wave + 4 * k;
+    if (mom) {
+      if (update) {
+        v[k] = fmaf(mu, v[k], u[k]);
+        if (r < rows && lane < cols) mom[(r0 + r) * l.m_row + c0 + lane] = v[k];
+      }
+      u[k] = ends.nesterov ? fmaf(mu, v[k], u[k]) : v[k];
+    }
+    if (turned_in) x[lane][r] = u[k];
+    else x[r][lane] = u[k];
+  }
+}
+
+struct Small { double *piece, *q; int side; };     // piece: [pieces, side, side]
+__device__ inline Small small_of(char* ws, const At& at, const EndArg& l) {
+  const int m = min(l.rows, l.cols), n = max(l.rows, l.cols), side = small_side(m);
+  double* base = (double*)(ws + at.l.ws + head_bytes(at.l.count)) + (int64_t)at.matrix * (pieces(n) + 1) * side * side;
+  return {base, base + (int64_t)pieces(n) * side * side, side};
+}
+
+// R x R elements of a 16 R square per thread: rows ty + 16 i, columns tx + 16 j.
+template <typename G, int R>
+__device__ inline void gram64(const Ends& ends, const EndArg& l, const At& at, const Small& w, float (*x)[kChunkStride]) {
+  const int n = max(l.rows, l.cols), chunks = (n + kChunk - 1) / kChunk, parts = pieces(n), tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  double acc[R][R] = {};
+  for (int c = at.unit; c < chunks; c += parts) {
+    __syncthreads();
+    load_chunk<G>(ends, l, at.matrix, true, c * kChunk, x);
+    __syncthreads();
+#pragma unroll 4
+    for (int k = 0; k < kChunk; ++k) {
+      double a[R], b[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) { a[i] = x[ty + 16 * i][k]; b[i] = x[tx + 16 * i][k]; }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = i; j < R; ++j) acc[i][j] = fma(a[i], b[j], acc[i][j]);
+    }
+  }
+  double* to = w.piece + (int64_t)at.unit * w.side * w.side;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int j = i; j < R; ++j) {
+      to[(ty + 16 * i) * w.side + tx + 16 * j] = acc[i][j];
+      if (j > i) to[(tx + 16 * j) * w.side + ty + 16 * i] = acc[i][j];
+    }
+}
+template <typename G>
+__global__ void __launch_bounds__(kThreads) k_gram64(Args c, Ends ends, char* ws) {
+  __shared__ float x[64][kChunkStride];
+  warm_args<576>();
   const At at = find(c);
   if (at.matrix < 0) return;
-  const Place p = place(at.l.mb, at.l.nb);
-  _Float16* base = halves_of(ws, at, p);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ib = wave >> 1, jb = wave & 1, inner = 2 * p.mb, words = p.mb * p.mb * 2 * kPair / 8;
-  const bool on = ib < p.mb && jb < p.mb;
-  const int place_to = (int)turned_at(jb, ib, p.mb);
-  for (int i = threadIdx.x; i < words; i += kThreads) ((f16x8*)sA)[i] = ((const f16x8*)(base + p.a))[i];
-  const StepFactors* step = head_of(ws, at).step + c.step;
-  __syncthreads();
-  // registers of f * left * right + g * right (kPoly: old = left = right)
-  const auto multiply = [&](const _Float16* left, const _Float16* right, const Factors& f, f32x4 (&v)[4]) {
-    Acc acc = {};
-    for (int k = 0; k < inner; ++k) acc.add(load_pair(left + (ib * inner + k) * kPair + lane * 8), load_pair(right + (jb * inner + k) * kPair + lane * 8));
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 before = value(get_turned(right + place_to + turned(q)));
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[q][r] = (acc.large[4 * q + r] + acc.small[4 * q + r]) * f.p0 * f.p1 + before[r] * f.old;
-    }
-  };
-  const auto write = [&](_Float16* to, const f32x4 (&v)[4]) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) put_turned(to + place_to + turned(q), split(v[q]));
-  };
-  for (int k = 0; k < steps; ++k) {
-    const StepFactors f = step[k];
-    f32x4 v[4];
-    if (on) {
-      multiply(sA, sA, f.poly, v);
-      write(sB, v);
-      if (k == 0) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = first_q(f.q, ib, jb, q, v[q]);
-        write(sQ, v);
-      }
-    }
-    __syncthreads();
-    if (k > 0) {
-      if (on) multiply(sB, sQ, f.q, v);
-      __syncthreads();
-      if (on) write(sQ, v);
-    }
-    if (k + 1 < steps) {
-      if (on) {
-        multiply(sB, sA, f.t, v);
-        write(sT, v);
-      }
-      __syncthreads();
-      if (on) {
-        multiply(sB, sT, f.next, v);
-        write(sA, v);
-      }
-    }
-    __syncthreads();
+  const EndArg l = ends.layer[at.layer];
+  const Small w = small_of(ws, at, l);
+  if (w.side == 16) gram64<G, 1>(ends, l, at, w, x);
+  else if (w.side == 32) gram64<G, 2>(ends, l, at, w, x);
+  else if (w.side == 48) gram64<G, 3>(ends, l, at, w, x);
+  else gram64<G, 4>(ends, l, at, w, x);
+}
+
+struct Coefs { int steps; float eps, coef[POP_NS_MAX_STEPS][3]; };
+constexpr int kSquareStride = 66;           // doubles of an LDS row: rows 16 apart in other banks
+template <int R>
+__device__ inline void square64(const Coefs& c, const Small& w, int parts, double (*s)[64 * kSquareStride]) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, side = w.side;
+  double *A = s[0], *B = s[1], *Q = s[2];
+  const auto at = [](int i, int j) { return i * kSquareStride + j; };
+  for (int e = threadIdx.x; e < side * side; e += kThreads) {
+    double v = 0.0;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) v += w.piece[(int64_t)p * side * side + e];
+    A[at(e / side, e % side)] = v;
   }
-  _Float16* to = base + p.q[c.done_parity];
-  for (int i = threadIdx.x; i < words; i += kThreads) ((f16x8*)to)[i] = ((const f16x8*)sQ)[i];
+  __syncthreads();
+  double norm2 = 0.0;
+  for (int i = 0; i < side; ++i) norm2 += A[at(i, i)];
+  const double inv = 1.0 / (sqrt(norm2) + (double)c.eps);
+  __syncthreads();
+  for (int e = threadIdx.x; e < side * side; e += kThreads) {
+    A[at(e / side, e % side)] *= inv * inv;
+    Q[at(e / side, e % side)] = e / side == e % side ? 1.0 : 0.0;
+  }
+  __syncthreads();
+  double v[R][R];
+  // left * right on and above the diagonal of blocks; both are symmetric
+  const auto multiply = [&](const double* left, const double* right) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < R; ++j) v[i][j] = 0.0;
+#pragma unroll 2
+    for (int k = 0; k < side; ++k) {
+      double a[R], b[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) { a[i] = left[at(k, ty + 16 * i)]; b[i] = right[at(k, tx + 16 * i)]; }
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = i; j < R; ++j) v[i][j] = fma(a[i], b[j], v[i][j]);
+    }
+  };
+  // f * product + g * old, in both triangles; `to` may be `old` or an operand (behind the barrier all have read it)
+  const auto write = [&](double* to, const double* old, double f, double g) {
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = i; j < R; ++j) v[i][j] = f * v[i][j] + g * old[at(ty + 16 * i, tx + 16 * j)];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = i; j < R; ++j) {
+        to[at(ty + 16 * i, tx + 16 * j)] = v[i][j];
+        if (j > i) to[at(tx + 16 * j, ty + 16 * i)] = v[i][j];
+      }
+    __syncthreads();
+  };
+  for (int k = 0; k < c.steps; ++k) {
+    const double k0 = c.coef[k][0], k1 = c.coef[k][1], k2 = c.coef[k][2];
+    multiply(A, A);
+    write(B, A, k2, k1);
+    multiply(B, Q);
+    write(Q, Q, 1.0, k0);
+    if (k + 1 == c.steps) break;
+    multiply(B, A);
+    write(A, A, 1.0, k0);                   // P A
+    multiply(B, A);
+    write(A, A, 1.0, k0);                   // P P A
+  }
+  for (int e = threadIdx.x; e < side * side; e += kThreads) w.q[e] = Q[at(e / side, e % side)] * inv;
+}
+__global__ void __launch_bounds__(kThreads) k_square64(Args c, Ends ends, Coefs coefs, char* ws) {
+  __shared__ double s[3][64 * kSquareStride];
+  warm_args<576>();
+  const At at = find(c);
+  if (at.matrix < 0) return;
+  const EndArg l = ends.layer[at.layer];
+  const Small w = small_of(ws, at, l);
+  const int parts = pieces(max(l.rows, l.cols));
+  if (w.side == 16) square64<1>(coefs, w, parts, s);
+  else if (w.side == 32) square64<2>(coefs, w, parts, s);
+  else if (w.side == 48) square64<3>(coefs, w, parts, s);
+  else square64<4>(coefs, w, parts, s);
+}
+
+// Q U for 64 columns of X; Q has 1 / (|U| + eps) in it.
+template <typename G>
+__global__ void __launch_bounds__(kThreads) k_last64(Args c, Ends ends, char* ws) {
+  __shared__ float x[64][kChunkStride];
+  __shared__ double q[64 * 64];
+  warm_args<576>();
+  const At at = find(c);
+  if (at.matrix < 0) return;
+  const EndArg l = ends.layer[at.layer];
+  const Small w = small_of(ws, at, l);
+  const bool turned_in = l.rows > l.cols;
+  const int m = min(l.rows, l.cols), n = max(l.rows, l.cols), j0 = at.unit * kChunk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  load_chunk<G>(ends, l, at.matrix, false, j0, x);
+  for (int e = threadIdx.x; e < w.side * w.side; e += kThreads) q[e] = w.q[e];
+  __syncthreads();
+  const float* hp = ends.hparams ? ends.hparams + 3 * at.matrix : nullptr;
+  const float up = hp ? -hp[0] * l.scale : 0.0f, keep = hp ? fmaf(-hp[0], hp[2], 1.0f) : 0.0f;
+  // lanes along the caller's columns: an element of row r and column `col` of its matrix
+  const int rows = turned_in ? min(n - j0, 64) : m, cols = turned_in ? m : min(n - j0, 64), r0 = turned_in ? j0 : 0, c0 = turned_in ? 0 : j0;
+  // and of sixteen rows per wavefront
+  const int first = wave * 16;
+  if (first >= rows) return;
+  double v[16] = {};
+  if (turned_in) {
+    for (int k = 0; k < m; ++k) {
+      const double a = q[k * w.side + min(lane, w.side - 1)];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] = fma(a, (double)x[k][first + r], v[r]);
+    }
+  } else {
+    for (int k = 0; k < m; ++k) {
+      const double a = x[k][lane];
+      const double* b = q + k * w.side + first;             // up to 15 doubles behind the square's last row: q has 64 x 64
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] = fma(a, b[r], v[r]);
+    }
+  }
+  if (lane >= cols) return;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (first + r >= rows) break;
+    const int64_t to = at.matrix * l.out_matrix + (int64_t)(r0 + first + r) * l.out_row + c0 + lane;
+    if (hp) ((float*)l.out)[to] = fmaf(up, (float)v[r], ((const float*)l.out)[to] * keep);
+    else ((G*)l.out)[to] = (G)(float)v[r];
+  }
 }
 
 // no steps: X itself
@@ -945,8 +1108,22 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     else ends.layer[k] = {l.g, l.g_matrix, l.g_row, nullptr, 0, 0, l.out, l.out_matrix, l.out_row, l.rows, l.cols, l.scale, 0};
   }
   Args a = {};
+  int blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? pieces(l.rows > l.cols ? l.rows : l.cols) : 0; });
+  if (blocks) {
+    Coefs coefs;
+    coefs.steps = c.steps;
+    coefs.eps = c.eps;
+    for (int k = 0; k < POP_NS_MAX_STEPS; ++k)
+      for (int i = 0; i < 3; ++i) coefs.coef[k][i] = c.coef[k][i];
+    k_gram64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+    blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 1 : 0; });
+    k_square64<<<dim3(blocks), kThreads, 0, stream>>>(a, ends, coefs, ws);
+    blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? ((l.rows > l.cols ? l.rows : l.cols) + kChunk - 1) / kChunk : 0; });
+    k_last64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+  }
   Bounds bounds;
   bounds.steps = c.steps;
+  bounds.segment = c.segment;
   bounds.most = c.most;
   for (int k = 0; k < POP_NS_MAX_STEPS; ++k) {
     for (int i = 0; i < 3; ++i) bounds.coef[k][i] = c.coef[k][i];
@@ -954,22 +1131,21 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     bounds.q_most[k] = c.q_most[k];
   }
   bounds.gain[POP_NS_MAX_STEPS] = c.gain[POP_NS_MAX_STEPS];
-  int blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return parts(l.rows, l.cols); });
+  blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? 0 : parts(l.rows, l.cols); });
+  if (blocks == 0) return hipGetLastError();
   k_norms<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
   if (c.steps == 0) {
     k_no_steps<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
     return hipGetLastError();
   }
-  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return (p.mb * p.nb + 3) / 4; });
+  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 0 : (p.mb * p.nb + 3) / 4; });
   k_start<G><<<dim3(blocks), kThreads, 0, stream>>>(a, bounds, ends, ws);
   const NoEnds none;
   const auto square = [](const Place& p, int m, int) { return p.mb <= kSmall ? 0 : tiles(m); };
-  for (int first = 0, xt = 0; first < c.steps; first += kNsSegment, xt ^= 1) {
-    const int last = (first + kNsSegment < c.steps ? first + kNsSegment : c.steps) - 1;
-    launch_product<kGram, float>(c, args_of(first, first, last, xt), none, ws, stream, [](const Place&, int m, int) { return tiles(m); });
-    Args small = args_of(first, first, last, xt);
-    blocks = lay_out(c, small, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 1 : 0; });
-    if (blocks) k_small<<<dim3(blocks), kThreads, 0, stream>>>(small, last - first + 1, ws);
+  const auto full = [](const Place& p, int m, int n) { return p.mb <= kSmall ? 0 : m * n; };
+  for (int first = 0, xt = 0; first < c.steps; first += c.segment, xt ^= 1) {
+    const int last = (first + c.segment < c.steps ? first + c.segment : c.steps) - 1;
+    launch_product<kGram, float>(c, args_of(first, first, last, xt), none, ws, stream, square);
     for (int k = first; k <= last; ++k) {
       const Args s = args_of(k, first, last, xt);
       launch_product<kPoly, float>(c, s, none, ws, stream, square);
@@ -977,7 +1153,6 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
       if (k < last) launch_product<kNext, float>(c, s, none, ws, stream, square);
     }
     const Args s = args_of(last, first, last, xt);
-    const auto full = [](const Place&, int m, int n) { return m * n; };
     if (last + 1 < c.steps) launch_product<kApply, float>(c, s, none, ws, stream, full);
     else launch_product<kLast, G>(c, s, ends, ws, stream, full);
   }
@@ -988,7 +1163,10 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
 }  // namespace
 
 int64_t ns_workspace_bytes(int count, int rows, int cols) {
-  return ns::head_bytes(count) + count * ns::place_of(rows, cols).size * 2;     // whole 2 KB blocks
+  const ns::Place p = ns::place_of(rows, cols);
+  const int side = ns::small_side(rows < cols ? rows : cols);
+  const int64_t per = p.mb <= ns::kSmall ? (int64_t)(ns::pieces(rows < cols ? cols : rows) + 1) * side * side * 8 : p.size * 2;
+  return ns::head_bytes(count) + count * per;        // of whole 2 KB
 }
 
 hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s) {

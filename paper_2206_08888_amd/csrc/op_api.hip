@@ -65,7 +65,7 @@ int check_workspace(void* p, int64_t have, int64_t need) {
   return POP_OK;
 }
 
-// NsCall::most, gain and q_most.  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
+// NsCall::most, gain and q_most (segment is set).  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
 // in s^2; p(s) / s at an end or where its derivative in s^2 is 0.
 void bounds_of(const pop_ns_config& c, NsCall& n) {
   double top = 1.0, gain = 1.0, in_segment = 1.0;
@@ -82,7 +82,7 @@ void bounds_of(const pop_ns_config& c, NsCall& n) {
     if (k2 != 0.0 && -k1 / (2 * k2) > 0.0 && -k1 / (2 * k2) < end) most = fmax(most, ratio(-k1 / (2 * k2)));
     top = next;
     gain *= most;
-    in_segment = (k % kNsSegment == 0 ? 1.0 : in_segment) * most;
+    in_segment = (k % n.segment == 0 ? 1.0 : in_segment) * most;
     n.q_most[k] = (float)fmin(in_segment, 1e30);
     n.most = (float)fmax(n.most, top);
     if (!(n.most <= kMostSingular)) return;
@@ -90,7 +90,7 @@ void bounds_of(const pop_ns_config& c, NsCall& n) {
   n.gain[c.steps] = (float)fmin(gain, 1e30);
 }
 
-int check_ns(const pop_ns_config* c, int32_t dtype, NsCall& n) {
+int check_ns(const pop_ns_config* c, int32_t dtype, int segment, NsCall& n) {
   if (!c) return fail_thread(POP_EINVAL, "config is NULL");
   if (c->steps < 0 || c->steps > POP_NS_MAX_STEPS) return fail_thread(POP_EINVAL, "steps must be 0 .. %d", (int)POP_NS_MAX_STEPS);
   if (!(c->eps >= 1e-30f && c->eps <= 1e30f)) return fail_thread(POP_EINVAL, "eps must be within 1e-30 .. 1e30");
@@ -99,6 +99,7 @@ int check_ns(const pop_ns_config* c, int32_t dtype, NsCall& n) {
     for (float v : c->coef[k])
       if (!isfinite(v)) return fail_thread(POP_EINVAL, "coefficients of step %d are not finite", k);
   n = NsCall{};
+  n.segment = segment;
   bounds_of(*c, n);
   if (!(n.most <= kMostSingular)) return fail_thread(POP_EUNSUPPORTED, "the coefficients let singular values of at most 1 grow beyond %g", kMostSingular);
   n.steps = c->steps;
@@ -238,7 +239,9 @@ int64_t pop_orthogonalize_workspace_bytes(int32_t count, int32_t rows, int32_t c
 int pop_orthogonalize(const pop_ns_config* cfg, int32_t count, int32_t rows, int32_t cols, int32_t dtype, const pop_matrices* g,
                       const pop_matrices* out, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   NsCall n;
-  int rc = check_ns(cfg, dtype, n);
+  // (the rule's reasons: k_orthogonalize.hip)
+  const int64_t side = rows < cols ? rows : cols, other = rows < cols ? cols : rows;
+  int rc = check_ns(cfg, dtype, dtype != POP_F32 && 2 * other >= 3 * side ? 3 : 1, n);
   if (rc != POP_OK || (rc = check_shape(count, rows, cols)) != POP_OK) return rc;
   if (!g || !out) return fail_thread(POP_EINVAL, "g or out is NULL");
   if ((rc = check_matrices(count, rows, cols, *g, "g", false, element_bytes(dtype))) != POP_OK ||
@@ -260,7 +263,7 @@ int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_lay
 int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype, int32_t nesterov,
                   const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   NsCall n;
-  int rc = check_ns(cfg, dtype, n);
+  int rc = check_ns(cfg, dtype, 1, n);
   if (rc != POP_OK) return rc;
   const int64_t need = muon_workspace(P, n_layers, layers);
   if (need < 0) return (int)need;

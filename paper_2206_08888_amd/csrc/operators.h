@@ -59,11 +59,11 @@ struct NsCall {
   float coef[POP_NS_MAX_STEPS][3];
   float most;                        // singular values that start within [0, 1] stay below this in every step,
   float gain[POP_NS_MAX_STEPS + 1];  // and within gain[k] of what they started from in front of step k
+  int segment;                       // steps taken in the space of X X^T before X itself is multiplied
   float q_most[POP_NS_MAX_STEPS];    // within which the steps of a segment up to step k multiply a singular value
   NsLayer layer[POP_MUON_MAX_LAYERS];
 };
 int64_t ns_workspace_bytes(int count, int rows, int cols);      // of one layer, a multiple of 256
-constexpr int kNsSegment = 3;        // steps taken in the space of X X^T before X itself is multiplied
 hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s);
 
 }  // namespace pop
