@@ -14,8 +14,9 @@
 // and results of 16 bits, whose rounding is 2e-4 or more, three where that is less work, from n = 1.5 m on (four 1024 x
 // 4096: 877 us, with one step 1286; 256 x 256: 114, with one 102).
 //
-// All matrices of a call advance together, a launch per product.  m up to 64 has a path of its own: the squares of A, Q and
-// so on fit a workgroup, and with everything in 64 bits all steps are one segment (below, k_gram64).
+// All matrices of a call advance together, a launch per product.  Calls whose matrices all have m up to 64 take a path of
+// their own: the squares of A, Q and so on fit a workgroup, and with everything in 64 bits all steps are one segment (below,
+// k_gram64).  (Beside larger matrices small ones cost nothing, and launches of their own would.)
 //
 // Products on v_mfma_f32_32x32x16_f16 from operands in two fp16 halves, x = hi + lo with 11 bits each, held in units
 // (powers of two, Units below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
@@ -41,7 +42,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPair = 1024;                 // halves of a hi and a lo block
-constexpr int kSmall = 2;                   // bands of m up to which a matrix takes the path in 64 bits
+constexpr int kSmall = 2;                   // bands of m up to which matrices can take the path in 64 bits
 
 // Where the arrays of one matrix lie, in halves from the start of its workspace.
 struct Place {
@@ -792,8 +793,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
 
 // The 64-bit path: k_gram64 updates the momentum and sums U U^T over a piece of n, k_square64 adds the pieces up (the trace
 // is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Vector instructions: their
-// 64-bit rate is that of the matrix ones.  Errors: the rounding of the result.  Three launches: 17 x 2000 FIG1 us, 8 of 64 x
-// 2048 FIG2, bound by the latency of three launches and, for m = 64, by the 17 products of one workgroup.
+// 64-bit rate is that of the matrix ones.  Errors: the rounding of the result.  Three launches: 8 of 17 x 2000 30 us (48 as
+// fp16 halves in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58), 57 of them the 17 products of one workgroup.
 
 constexpr int kChunk = 64, kChunkStride = 65;
 // U's columns (of X) j0 .. j0 + 63 to LDS, zeros outside; `update`: with the momentum's step.
@@ -835,35 +836,27 @@ __device__ inline Small small_of(char* ws, const At& at, const EndArg& l) {
   return {base, base + (int64_t)pieces(n) * side * side, side};
 }
 
-// R x R elements of a 16 R square per thread: rows ty + 16 i, columns tx + 16 j.
-template <typename G, int R>
-__device__ inline void gram64(const Ends& ends, const EndArg& l, const At& at, const Small& w, float (*x)[kChunkStride]) {
-  const int n = max(l.rows, l.cols), chunks = (n + kChunk - 1) / kChunk, parts = pieces(n), tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  double acc[R][R] = {};
-  for (int c = at.unit; c < chunks; c += parts) {
-    __syncthreads();
-    load_chunk<G>(ends, l, at.matrix, true, c * kChunk, x);
-    __syncthreads();
-#pragma unroll 4
-    for (int k = 0; k < kChunk; ++k) {
-      double a[R], b[R];
+// Squares of up to 4 x 4 tiles on v_mfma_f64_16x16x4_f64: lane l supplies row (column) l & 15 of index l >> 4, and register r of
+// the result is element (4 r + (l >> 4), l & 15) of the tile.  The tiles on and above the diagonal go round the wavefronts, at
+// most three to each.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr int kMine = 3;
+struct Tiles { int i[kMine], j[kMine], n; };
+// Tiles `wave`, `wave` + waves, .. of `count` times the triangle.
+__device__ inline Tiles tiles_of(int side, int waves, int count) {
+  const int t = side / 16, wave = threadIdx.x >> 6, per = tiles(t);
+  Tiles m = {};
 #pragma unroll
-      for (int i = 0; i < R; ++i) { a[i] = x[ty + 16 * i][k]; b[i] = x[tx + 16 * i][k]; }
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int j = i; j < R; ++j) acc[i][j] = fma(a[i], b[j], acc[i][j]);
+  for (int s = 0; s < kMine; ++s) {
+    const int u = wave + s * waves;
+    if (u < count * per) {
+      triangle(t, u % per, m.i[s], m.j[s]);
+      ++m.n;
     }
   }
-  double* to = w.piece + (int64_t)at.unit * w.side * w.side;
-#pragma unroll
-  for (int i = 0; i < R; ++i)
-#pragma unroll
-    for (int j = i; j < R; ++j) {
-      to[(ty + 16 * i) * w.side + tx + 16 * j] = acc[i][j];
-      if (j > i) to[(tx + 16 * j) * w.side + ty + 16 * i] = acc[i][j];
-    }
+  return m;
 }
+
 template <typename G>
 __global__ void __launch_bounds__(kThreads) k_gram64(Args c, Ends ends, char* ws) {
   __shared__ float x[64][kChunkStride];
@@ -872,95 +865,128 @@ __global__ void __launch_bounds__(kThreads) k_gram64(Args c, Ends ends, char* ws
   if (at.matrix < 0) return;
   const EndArg l = ends.layer[at.layer];
   const Small w = small_of(ws, at, l);
-  if (w.side == 16) gram64<G, 1>(ends, l, at, w, x);
-  else if (w.side == 32) gram64<G, 2>(ends, l, at, w, x);
-  else if (w.side == 48) gram64<G, 3>(ends, l, at, w, x);
-  else gram64<G, 4>(ends, l, at, w, x);
+  const int n = max(l.rows, l.cols), chunks = (n + kChunk - 1) / kChunk, parts = pieces(n), lane = threadIdx.x & 63;
+  const Tiles mine = tiles_of(w.side, 4, 1);
+  f64x4 acc[kMine] = {};
+  for (int p = at.unit; p < chunks; p += parts) {
+    __syncthreads();
+    load_chunk<G>(ends, l, at.matrix, true, p * kChunk, x);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kMine; ++t) {
+      if (t >= mine.n) break;
+      const float *a = &x[16 * mine.i[t] + (lane & 15)][lane >> 4], *b = &x[16 * mine.j[t] + (lane & 15)][lane >> 4];
+#pragma unroll
+      for (int k = 0; k < kChunk; k += 4) acc[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)a[k], (double)b[k], acc[t], 0, 0, 0);
+    }
+  }
+  double* to = w.piece + (int64_t)at.unit * w.side * w.side;
+#pragma unroll
+  for (int t = 0; t < kMine; ++t) {
+    if (t >= mine.n) break;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = 16 * mine.i[t] + 4 * r + (lane >> 4), j = 16 * mine.j[t] + (lane & 15);
+      to[i * w.side + j] = acc[t][r];
+      if (mine.i[t] != mine.j[t]) to[j * w.side + i] = acc[t][r];
+    }
+  }
 }
 
 struct Coefs { int steps; float eps, coef[POP_NS_MAX_STEPS][3]; };
-constexpr int kSquareStride = 66;           // doubles of an LDS row: rows 16 apart in other banks
-template <int R>
-__device__ inline void square64(const Coefs& c, const Small& w, int parts, double (*s)[64 * kSquareStride]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, side = w.side;
-  double *A = s[0], *B = s[1], *Q = s[2];
-  const auto at = [](int i, int j) { return i * kSquareStride + j; };
-  for (int e = threadIdx.x; e < side * side; e += kThreads) {
-    double v = 0.0;
-#pragma unroll 8
-    for (int p = 0; p < parts; ++p) v += w.piece[(int64_t)p * side * side + e];
-    A[at(e / side, e % side)] = v;
-  }
-  __syncthreads();
-  double norm2 = 0.0;
-  for (int i = 0; i < side; ++i) norm2 += A[at(i, i)];
-  const double inv = 1.0 / (sqrt(norm2) + (double)c.eps);
-  __syncthreads();
-  for (int e = threadIdx.x; e < side * side; e += kThreads) {
-    A[at(e / side, e % side)] *= inv * inv;
-    Q[at(e / side, e % side)] = e / side == e % side ? 1.0 : 0.0;
-  }
-  __syncthreads();
-  double v[R][R];
-  // left * right on and above the diagonal of blocks; both are symmetric
-  const auto multiply = [&](const double* left, const double* right) {
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int j = 0; j < R; ++j) v[i][j] = 0.0;
-#pragma unroll 2
-    for (int k = 0; k < side; ++k) {
-      double a[R], b[R];
-#pragma unroll
-      for (int i = 0; i < R; ++i) { a[i] = left[at(k, ty + 16 * i)]; b[i] = right[at(k, tx + 16 * i)]; }
-#pragma unroll
-      for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int j = i; j < R; ++j) v[i][j] = fma(a[i], b[j], v[i][j]);
-    }
-  };
-  // f * product + g * old, in both triangles; `to` may be `old` or an operand (behind the barrier all have read it)
-  const auto write = [&](double* to, const double* old, double f, double g) {
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int j = i; j < R; ++j) v[i][j] = f * v[i][j] + g * old[at(ty + 16 * i, tx + 16 * j)];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int j = i; j < R; ++j) {
-        to[at(ty + 16 * i, tx + 16 * j)] = v[i][j];
-        if (j > i) to[at(tx + 16 * j, ty + 16 * i)] = v[i][j];
-      }
-    __syncthreads();
-  };
-  for (int k = 0; k < c.steps; ++k) {
-    const double k0 = c.coef[k][0], k1 = c.coef[k][1], k2 = c.coef[k][2];
-    multiply(A, A);
-    write(B, A, k2, k1);
-    multiply(B, Q);
-    write(Q, Q, 1.0, k0);
-    if (k + 1 == c.steps) break;
-    multiply(B, A);
-    write(A, A, 1.0, k0);                   // P A
-    multiply(B, A);
-    write(A, A, 1.0, k0);                   // P P A
-  }
-  for (int e = threadIdx.x; e < side * side; e += kThreads) w.q[e] = Q[at(e / side, e % side)] * inv;
-}
-__global__ void __launch_bounds__(kThreads) k_square64(Args c, Ends ends, Coefs coefs, char* ws) {
-  __shared__ double s[3][64 * kSquareStride];
+constexpr int kSquareStride = 72;           // doubles of an LDS row: four rows of 16 meet every bank twice
+constexpr int kSquareThreads = 512;
+__global__ void __launch_bounds__(kSquareThreads) k_square64(Args c, Ends ends, Coefs coefs, char* ws) {
+  __shared__ double A[64 * kSquareStride], B[64 * kSquareStride], Q[64 * kSquareStride];
   warm_args<576>();
   const At at = find(c);
   if (at.matrix < 0) return;
   const EndArg l = ends.layer[at.layer];
   const Small w = small_of(ws, at, l);
-  const int parts = pieces(max(l.rows, l.cols));
-  if (w.side == 16) square64<1>(coefs, w, parts, s);
-  else if (w.side == 32) square64<2>(coefs, w, parts, s);
-  else if (w.side == 48) square64<3>(coefs, w, parts, s);
-  else square64<4>(coefs, w, parts, s);
+  const int parts = pieces(max(l.rows, l.cols)), side = w.side, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = kSquareThreads / 64;
+  const auto element = [](int i, int j) { return i * kSquareStride + j; };
+  for (int e = threadIdx.x; e < side * side; e += kSquareThreads) {
+    double v = 0.0;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) v += w.piece[(int64_t)p * side * side + e];
+    A[element(e / side, e % side)] = v;
+  }
+  __syncthreads();
+  double norm2 = 0.0;
+  for (int i = 0; i < side; ++i) norm2 += A[element(i, i)];
+  const double inv = 1.0 / (sqrt(norm2) + (double)coefs.eps);
+  __syncthreads();
+  for (int e = threadIdx.x; e < side * side; e += kSquareThreads) {
+    A[element(e / side, e % side)] *= inv * inv;
+    Q[element(e / side, e % side)] = e / side == e % side ? 1.0 : 0.0;
+  }
+  __syncthreads();
+  // A product of two of the (symmetric) squares, tile by tile: f * left * right + g * old, in both triangles of `to`, which may
+  // be `old` or an operand (behind the barrier all have read it).  A wavefront's tiles take turns, so that no
+  // instruction waits for the one before it, with the operands of 16 indices read ahead of them.
+  struct Task { const double *left, *right, *old; double *to, f, g; };
+  const auto phase = [&](const Tiles& mine, const Task (&task)[kMine]) {
+    f64x4 v[kMine];
+    const double *a[kMine], *b[kMine];
+#pragma unroll
+    for (int t = 0; t < kMine; ++t) {
+      v[t] = f64x4{};
+      a[t] = task[t].left + element(lane >> 4, 16 * mine.i[t] + (lane & 15));
+      b[t] = task[t].right + element(lane >> 4, 16 * mine.j[t] + (lane & 15));
+    }
+    const auto over = [&](auto count) {
+      for (int k = 0; k < side; k += 16) {
+        double x[kMine][4], y[kMine][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int t = 0; t < decltype(count)::value; ++t) {
+            x[t][q] = a[t][(k + 4 * q) * kSquareStride];
+            y[t][q] = b[t][(k + 4 * q) * kSquareStride];
+          }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int t = 0; t < decltype(count)::value; ++t) v[t] = __builtin_amdgcn_mfma_f64_16x16x4f64(x[t][q], y[t][q], v[t], 0, 0, 0);
+      }
+#pragma unroll
+      for (int t = 0; t < decltype(count)::value; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          v[t][r] = task[t].f * v[t][r] + task[t].g * task[t].old[element(16 * mine.i[t] + 4 * r + (lane >> 4), 16 * mine.j[t] + (lane & 15))];
+    };
+    if (mine.n == 3) over(std::integral_constant<int, 3>());
+    else if (mine.n == 2) over(std::integral_constant<int, 2>());
+    else if (mine.n == 1) over(std::integral_constant<int, 1>());
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kMine; ++t)
+      if (t < mine.n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * mine.i[t] + 4 * r + (lane >> 4), j = 16 * mine.j[t] + (lane & 15);
+          task[t].to[element(i, j)] = v[t][r];
+          if (mine.i[t] != mine.j[t]) task[t].to[element(j, i)] = v[t][r];
+        }
+    __syncthreads();
+  };
+  const int per = tiles(side / 16);
+  const Tiles one = tiles_of(side, waves, 1), two = tiles_of(side, waves, 2);
+  for (int k = 0; k < coefs.steps; ++k) {
+    const double k0 = coefs.coef[k][0], k1 = coefs.coef[k][1], k2 = coefs.coef[k][2];
+    const Task poly = {A, A, A, B, k2, k1}, q = {B, Q, Q, Q, 1.0, k0}, next = {B, A, A, A, 1.0, k0};
+    phase(one, {poly, poly, poly});
+    if (k + 1 == coefs.steps) {
+      phase(one, {q, q, q});
+      break;
+    }
+    Task both[kMine];                       // Q = P Q, and A = P A of the second triangle
+#pragma unroll
+    for (int s = 0; s < kMine; ++s) both[s] = wave + s * waves < per ? q : next;
+    phase(two, both);
+    phase(one, {next, next, next});         // A = P P A
+  }
+  for (int e = threadIdx.x; e < side * side; e += kSquareThreads) w.q[e] = Q[element(e / side, e % side)] * inv;
 }
 
 // Q U for 64 columns of X; Q has 1 / (|U| + eps) in it.
@@ -1108,18 +1134,22 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     else ends.layer[k] = {l.g, l.g_matrix, l.g_row, nullptr, 0, 0, l.out, l.out_matrix, l.out_row, l.rows, l.cols, l.scale, 0};
   }
   Args a = {};
-  int blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? pieces(l.rows > l.cols ? l.rows : l.cols) : 0; });
-  if (blocks) {
+  int blocks;
+  bool small = true;
+  for (int k = 0; k < c.n_layers; ++k) small = small && place_of(c.layer[k].rows, c.layer[k].cols).mb <= kSmall;
+  if (small) {
     Coefs coefs;
     coefs.steps = c.steps;
     coefs.eps = c.eps;
     for (int k = 0; k < POP_NS_MAX_STEPS; ++k)
       for (int i = 0; i < 3; ++i) coefs.coef[k][i] = c.coef[k][i];
+    blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return pieces(l.rows > l.cols ? l.rows : l.cols); });
     k_gram64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
-    blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 1 : 0; });
-    k_square64<<<dim3(blocks), kThreads, 0, stream>>>(a, ends, coefs, ws);
-    blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? ((l.rows > l.cols ? l.rows : l.cols) + kChunk - 1) / kChunk : 0; });
+    blocks = lay_out(c, a, [](const NsLayer&, const Place&) { return 1; });
+    k_square64<<<dim3(blocks), kSquareThreads, 0, stream>>>(a, ends, coefs, ws);
+    blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return ((l.rows > l.cols ? l.rows : l.cols) + kChunk - 1) / kChunk; });
     k_last64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
+    return hipGetLastError();
   }
   Bounds bounds;
   bounds.steps = c.steps;
@@ -1131,18 +1161,17 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     bounds.q_most[k] = c.q_most[k];
   }
   bounds.gain[POP_NS_MAX_STEPS] = c.gain[POP_NS_MAX_STEPS];
-  blocks = lay_out(c, a, [](const NsLayer& l, const Place& p) { return p.mb <= kSmall ? 0 : parts(l.rows, l.cols); });
-  if (blocks == 0) return hipGetLastError();
+  blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return parts(l.rows, l.cols); });
   k_norms<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
   if (c.steps == 0) {
     k_no_steps<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
     return hipGetLastError();
   }
-  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return p.mb <= kSmall ? 0 : (p.mb * p.nb + 3) / 4; });
+  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return (p.mb * p.nb + 3) / 4; });
   k_start<G><<<dim3(blocks), kThreads, 0, stream>>>(a, bounds, ends, ws);
   const NoEnds none;
-  const auto square = [](const Place& p, int m, int) { return p.mb <= kSmall ? 0 : tiles(m); };
-  const auto full = [](const Place& p, int m, int n) { return p.mb <= kSmall ? 0 : m * n; };
+  const auto square = [](const Place&, int m, int) { return tiles(m); };
+  const auto full = [](const Place&, int m, int n) { return m * n; };
   for (int first = 0, xt = 0; first < c.steps; first += c.segment, xt ^= 1) {
     const int last = (first + c.segment < c.steps ? first + c.segment : c.steps) - 1;
     launch_product<kGram, float>(c, args_of(first, first, last, xt), none, ws, stream, square);
@@ -1165,8 +1194,8 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
 int64_t ns_workspace_bytes(int count, int rows, int cols) {
   const ns::Place p = ns::place_of(rows, cols);
   const int side = ns::small_side(rows < cols ? rows : cols);
-  const int64_t per = p.mb <= ns::kSmall ? (int64_t)(ns::pieces(rows < cols ? cols : rows) + 1) * side * side * 8 : p.size * 2;
-  return ns::head_bytes(count) + count * per;        // of whole 2 KB
+  const int64_t small = p.mb <= ns::kSmall ? (int64_t)(ns::pieces(rows < cols ? cols : rows) + 1) * side * side * 8 : 0;
+  return ns::head_bytes(count) + count * (p.size * 2 > small ? p.size * 2 : small);        // of whole 2 KB
 }
 
 hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s) {
