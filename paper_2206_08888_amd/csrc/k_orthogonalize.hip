@@ -570,24 +570,21 @@ __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
   if constexpr (MODE == kLast) {
     write_result<G>(ends, at, ib, jb, wave, weights, v);
   } else {
-    Quad h = split(v);
-    put_turned(o.to + place_to, h);
-    const bool mirrored = MODE == kApply || ib != jb;
+    const bool mirrored = MODE == kApply || ib != jb, q_alone = MODE == kPoly && c.first_step && c.last_step;
     const int64_t mirror_to = pair_at(ib, 2 * jb + wave, MODE == kApply ? p.nb : p.mb);
-    if (mirrored) {
+    const auto write = [&](_Float16* to, _Float16* mirror) {
+      const Quad h = split(v);
+      put_turned(to + place_to, h);
+      if (!mirrored) return;
+      __syncthreads();                        // (of a block before)
       stage(scratch, wave, h);
       __syncthreads();
-      if (wave < 2) put(o.mirror + mirror_to, scratch, wave);
-    }
+      if (wave < 2) put(mirror + mirror_to, scratch, wave);
+    };
+    if (!q_alone) write(o.to, o.mirror);
     if (MODE == kPoly && c.first_step) {
-      h = split(first_q(fq, ib, jb, wave, v));
-      put_turned(base + p.q[0] + place_to, h);
-      if (mirrored) {
-        __syncthreads();
-        stage(scratch, wave, h);
-        __syncthreads();
-        if (wave < 2) put(base + p.q[0] + mirror_to, scratch, wave);
-      }
+      v = first_q(fq, ib, jb, wave, v);
+      write(base + p.q[0], base + p.q[0]);
     }
   }
 }
@@ -779,7 +776,8 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
 #pragma unroll
         for (int q = 0; q < 4; ++q) write_result<G>(ends, at, ib, jb, q, weights[q], v[q]);
       } else {
-        write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, scratch);
+        if (!(MODE == kPoly && c.first_step && c.last_step))        // a segment of one step: only Q is used
+          write_block(v, o.to + place_to, mirrored ? o.mirror + mirror_to : nullptr, scratch);
         if (MODE == kPoly && c.first_step) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] = first_q(fq, ib, jb, q, v[q]);
