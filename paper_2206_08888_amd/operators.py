@@ -69,6 +69,9 @@ def _dtype_code(dtype):
     return DTYPE_CODES[dtype]
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream         # current_stream(index).cuda_stream without the object around it
+
+
 class _Operator:
     """Device and type checks, and the stream of a call.  Calls are short beside their launches, so the checks take the
     shortest way through what is right and find out what is wrong afterwards."""
@@ -107,10 +110,10 @@ class _Operator:
     def _call(self, fn, *args):
         """Enqueue on the current stream of this operator's device."""
         if torch.cuda.current_device() == self.index:
-            rc = fn(*args, torch.cuda.current_stream(self.index).cuda_stream)
+            rc = fn(*args, _raw_stream(self.index))
         else:
             with torch.cuda.device(self.device):
-                rc = fn(*args, torch.cuda.current_stream(self.index).cuda_stream)
+                rc = fn(*args, _raw_stream(self.index))
         if rc:
             _check(rc)
 
