@@ -394,6 +394,7 @@ typedef struct {
 int64_t pop_recurrence_workspace_bytes(const pop_recurrence_config* cfg);
 int64_t pop_recurrence_states_bytes(const pop_recurrence_config* cfg);
 
+/* POP_EUNSUPPORTED, as by the backward pass, for more than 2^28 sequences times channels. */
 int pop_recurrence_forward(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
                            void* workspace, int64_t workspace_bytes, void* hip_stream);
 
@@ -414,7 +415,8 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  *   X = G / (|G| + eps);   `steps` times:  A = X X^T,  X = k0 X + (k1 A + k2 A A) X         (Newton-Schulz products)
  *
  * which drives the singular values of G towards 1.  All sums are fp32 (|G|: fp64).  Products run on the fp16 matrix
- * instructions from operands split into two halves of 11 bits each, which is fp32's precision up to the last bits. */
+ * instructions from operands split into two halves of 11 bits each, which is fp32's precision up to the last bits; calls
+ * whose matrices all have at most 64 rows or at most 64 columns run in fp64. */
 enum { POP_NS_MAX_STEPS = 16 };
 typedef struct {
   int32_t steps;                        /* 0 .. POP_NS_MAX_STEPS */

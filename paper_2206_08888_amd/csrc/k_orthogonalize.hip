@@ -790,9 +790,11 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
 // ---- m <= 64, in 64 bits
 
 // The 64-bit path: k_gram64 updates the momentum and sums U U^T over a piece of n, k_square64 adds the pieces up (the trace
-// is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Vector instructions: their
-// 64-bit rate is that of the matrix ones.  Errors: the rounding of the result.  Three launches: 8 of 17 x 2000 30 us (48 as
-// fp16 halves in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58), 57 of them the 17 products of one workgroup.
+// is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Errors: the rounding
+// of the result.  Three launches, in which k_square64's products, one after the other in one workgroup per matrix, are the
+// longest part: 8 of 17 x 2000 30 us (48 as fp16 halves in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58).
+// That part on vector instructions made it 119, on the matrix ones with a wavefront's tiles one by one 159, its chains
+// interleaved 92, from eight wavefronts 77.
 
 constexpr int kChunk = 64, kChunkStride = 65;
 // U's columns (of X) j0 .. j0 + 63 to LDS, zeros outside; `update`: with the momentum's step.

@@ -14,9 +14,10 @@
 // their steps again from the state in front of them: every element is read once and its gate computed once.  Wavefronts
 // whose steps all exist and have no resets among them skip what is for those.
 //
-// Where the columns do not fill the chip, sequences are shared by several workgroups: of up to kChainMost tiles each
-// tile has a workgroup of its own that waits for the state of the one before (kChain); longer ones are cut into segments
-// whose maps a launch of its own finds (kMaps, kSegments), at the price of reading x and g twice.
+// Where the columns do not fill the chip, sequences are shared by several workgroups: each tile has a workgroup of its own
+// that waits for the state of the one before (kChain), or, where columns are so few that this wait would be the longest part,
+// sequences are cut into segments whose maps a launch of its own finds (kMaps, kSegments), at the price of reading x and g
+// twice.
 #include <hip/hip_runtime.h>
 #include "operators.h"
 
@@ -203,6 +204,10 @@ template <int V> __device__ inline void bias_of(const RecurArgs& a, const Lane& 
 
 // ---- forward
 
+// Bound by memory: x, g and y once, 3 elements a step and column.  kWhole, 80 agents of 8 x 512 steps x 256 columns in bf16:
+// 122 us, 4.2 TB/s (a large copy: 4.8).  kChain, 10 agents of 4 x 1000 x 256 in fp32: 28 us, 4.3 TB/s, behind 3 of the
+// clearing launch.  kMaps + kSegments, one sequence of 65536 x 256 in bf16: 16 + 25 us at 4.1 TB/s, two thirds of it x and g
+// twice.  Single elements (V = 1, odd strides): 23 agents of 3 x 777 x 129 in fp32, half of the steps behind the ends: 24 us.
 template <typename E, int V, int N, int MODE>
 __global__ void __launch_bounds__(8192 / N) k_forward(RecurArgs a, int chunks, int per, int segments) {
   using S = Shape<E, V, N>;
@@ -334,7 +339,7 @@ __global__ void __launch_bounds__(kThreads) k_no_steps(const float* from, float*
 
 // ---- backward
 
-// A segment's map of the gradient behind it to the one in front of it.
+// A segment's map of the gradient behind it to the one in front of it: g and dy are read, 5.0 TB/s.
 template <typename E, int V, int N>
 __global__ void __launch_bounds__(8192 / N) k_backward_maps(RecurArgs a, int chunks, int per, int segments) {
   using S = Shape<E, V, N>;
@@ -408,7 +413,11 @@ __global__ void __launch_bounds__(8192 / N) k_backward_maps(RecurArgs a, int chu
   }
 }
 
-// dx and dg, and the sums of dg over the segment to `sums` [segments, columns].
+// dx and dg, and the sums of dg over the segment to `sums` [segments, columns].  States are found again from those in front
+// of the tiles, at an LDS walk's cost; gates too: kept ones would be another array to write and read.  Bound by memory, 5
+// elements a step and column: 80 agents of 8 x 512 x 256 in bf16 199 us, 4.2 TB/s; 2 of 2 x 16383 x 512 in fp16 75 us, 4.5,
+// behind 27 for the maps.  The chain (23 agents of 3 x 777 x 129, fp32, single elements, ragged: 36 us) also waits for its
+// hand-overs.
 template <typename E, int V, int N, int MODE>
 __global__ void __launch_bounds__(8192 / N, 2) k_backward(RecurArgs a, int chunks, int per, int segments, float* sums) {
   using S = Shape<E, V, N>;
@@ -610,7 +619,8 @@ __global__ void __launch_bounds__(kThreads) k_bias_sum(const float* sums, float*
 
 // ---- single steps
 
-// V channels of a row per lane.
+// V channels of a row per lane; memory's latency for few rows (10 of 256 channels: 2.8 us), its rate for many (80 agents of
+// 256 rows x 256 in bf16: 11.8 us, 73 MB at 6.2 TB/s, which the Infinity Cache gives and HBM would not).
 template <typename E, int V>
 __global__ void __launch_bounds__(kThreads) k_step(RecurArgs a) {
   typedef typename Vec<E, V>::type vec;
@@ -643,18 +653,28 @@ __global__ void __launch_bounds__(kThreads) k_step(RecurArgs a) {
 unsigned blocks(int64_t n) { return (unsigned)((n + kThreads - 1) / kThreads); }
 
 // Elements of a tile per lane: workgroups of 256 threads for 32, of 512 for 16.  The forward kernels of long sequences are
-// ahead with 32 (forward_1_agent_long 41.1 us, with 16 43.0; train_80_agents 321 / 328), chains, whose tiles wait for each
-// other, with 16 (10 agents of 4 x 1000 steps 31.3 / 34.2); the backward kernel holds twice as much per element, with 32 it
-// spills (train_80_agents 552), and with 8 gains nothing (333).
+// ahead with 32 (one sequence of 65536 x 256 41.1 us, with 16 43.0; with its backward pass, 80 agents of 8 x 512 x 256 321 /
+// 328), chains, whose tiles wait for each other, with 16 (10 agents of 4 x 1000 x 256 31.3 / 34.2); the backward kernel holds
+// twice as much per element, with 32 it spills (80 agents: 552), and with 8 gains nothing (333).
 constexpr int kElements = 32, kElementsChain = 16, kElementsBack = 16;
 
-// Sequences are shared where their columns alone do not fill the chip.
+// How sequences are shared, by groups of 64 columns and tiles of 128 steps; us of a forward and a backward pass.
+// kWhole from 256 groups on, where the columns alone fill the chip: 256 groups of 4 tiles in bf16 39, as chains 55; 512 of 16
+// 222 / 308; 2560 of 4 290 / 383; fp32 256 of 4 53 / 65.  But in fp32, where such calls are bound by memory alone, chains,
+// whose workgroups are many and short, leave no CU idle at the end: 320 groups of 16 tiles 263, whole 321; 640 of 8 261 / 286;
+// 2560 of 8 982 / 1047 (512 of 8: 224 / 220; 256 of 8: 117 / 104).
+// A chain takes 1.25 us a tile from one workgroup to the next, segments read two thirds more: with few columns segments
+// are ahead, from 64 groups in fp32 (128 of 16 bits) on chains.  fp32, 32 groups of 16 tiles: chains 67, segments 47; of
+// 32: 106 / 92; 64 of 16: 75 / 90; of 128: 463 / 631; bf16, 64 of 16: 66 / 61; of 128: 376 / 337; 128 of 16: 88 / 96; of 128:
+// 595 / 661.
 struct Cut { int mode, chunks, per, segments; };
-constexpr int kMaxSegments = 128, kChainMost = 24;
-Cut cut_of(int64_t P, int64_t B, int64_t T, int64_t C) {
+constexpr int kMaxSegments = 128, kWholeFrom = 256, kChainBytesFrom = 256, kWholeTiles = 8;
+constexpr int64_t kChainTilesMost = 1 << 22; // workgroups of 512 work items, below 2^32 in all
+Cut cut_of(int64_t P, int64_t B, int64_t T, int64_t C, int64_t element) {
   const int64_t groups = (P * B * C + kColumns - 1) / kColumns, chunks = recur_chunks(T);
-  if (groups >= 512 || chunks <= 1) return {kWhole, (int)chunks, (int)chunks, 1};
-  if (chunks <= kChainMost) return {kChain, (int)chunks, 1, (int)chunks};
+  const bool chains = groups * chunks <= kChainTilesMost;
+  if (chunks <= 1 || (groups >= kWholeFrom && (element == 2 || chunks < kWholeTiles || !chains))) return {kWhole, (int)chunks, (int)chunks, 1};
+  if (chains && groups * element >= kChainBytesFrom) return {kChain, (int)chunks, 1, (int)chunks};
   int64_t want = (1024 + groups - 1) / groups;
   if (want > kMaxSegments) want = kMaxSegments;
   if (want > chunks) want = chunks;
@@ -694,8 +714,8 @@ template <typename E> hipError_t forward(const RecurArgs& a, hipStream_t s) {
     if (a.h_last) k_no_steps<<<blocks(n), kThreads, 0, s>>>(a.h0, a.h_last, n);
     return hipGetLastError();
   }
-  const Cut c = cut_of(a.P, a.B, a.T, a.C);
   const int64_t e = sizeof(E);
+  const Cut c = cut_of(a.P, a.B, a.T, a.C, e);
   if (a.C % 4 == 0 && wide(a.x, e) && wide(a.g, e) && wide(a.y, e)) forward<E, 4>(a, c, n, s);
   else forward<E, 1>(a, c, n, s);
   return hipGetLastError();
@@ -720,8 +740,8 @@ template <typename E> hipError_t backward(const RecurArgs& a, hipStream_t s) {
     if (a.dbias) k_no_steps<<<blocks(nb), kThreads, 0, s>>>(nullptr, a.dbias, nb);
     return hipGetLastError();
   }
-  const Cut c = cut_of(a.P, a.B, a.T, a.C);
   const int64_t e = sizeof(E);
+  const Cut c = cut_of(a.P, a.B, a.T, a.C, e);
   float* sums = a.ws + 2 * (n * c.segments + 1);
   if (a.C % 4 == 0 && wide(a.x, e) && wide(a.g, e) && wide(a.dy, e) && wide(a.dx, e) && wide(a.dg, e)) backward<E, 4>(a, c, n, sums, s);
   else backward<E, 1>(a, c, n, sums, s);
@@ -742,9 +762,9 @@ template <typename E> hipError_t step(const RecurArgs& a, hipStream_t s) {
 }  // namespace recur
 }  // namespace
 
-int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C) { 
-  return T == 0 ? 0 : 3 * P * B * C * recur::cut_of(P, B, T, C).segments + 2;   // maps or words (and the ticket), sums
- }
+int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C, int64_t element) {
+  return T == 0 ? 0 : 3 * P * B * C * recur::cut_of(P, B, T, C, element).segments + 2;   // maps or words (and the ticket), sums
+}
 
 hipError_t launch_recur_forward(const RecurArgs& a, int dtype, hipStream_t s) {
   return dtype == POP_F32 ? recur::forward<float>(a, s) : dtype == POP_BF16 ? recur::forward<__bf16>(a, s) : recur::forward<_Float16>(a, s);

@@ -8,7 +8,8 @@ namespace pop {
 namespace op {
 
 constexpr int64_t kAlignment = 256;          // of a workspace
-constexpr int64_t kMaxLanes = 1ll << 31;     // a launch's work items per grid dimension stay below 2^32
+// a launch's work items per grid dimension stay below 2^32: one per column in a single step, up to eight over sequences
+constexpr int64_t kMaxLanes = 1ll << 31, kMaxColumns = 1ll << 28;
 constexpr int kMaxSteps = 1 << 22;           // chunks of a sequence are a grid dimension of at most 65,535
 
 constexpr double kMostSingular = 8.0;
@@ -21,6 +22,11 @@ int check_recurrence(const pop_recurrence_config* c) {
   if (c->dtype != POP_F32 && c->dtype != POP_BF16 && c->dtype != POP_F16) return fail_thread(POP_EINVAL, "config: unknown dtype %d", c->dtype);
   if ((int64_t)c->P * c->batch >= kMaxLanes / c->C) return fail_thread(POP_EUNSUPPORTED, "P * batch * C must be below 2^31");
   if (c->T > kMaxSteps) return fail_thread(POP_EUNSUPPORTED, "T must be at most %d", kMaxSteps);
+  return POP_OK;
+}
+
+int check_columns(const pop_recurrence_config* c) {
+  if ((int64_t)c->P * c->batch * c->C > kMaxColumns) return fail_thread(POP_EUNSUPPORTED, "P * batch * C must be at most 2^28 but for single steps");
   return POP_OK;
 }
 
@@ -168,7 +174,7 @@ extern "C" {
 
 int64_t pop_recurrence_workspace_bytes(const pop_recurrence_config* cfg) {
   const int rc = check_recurrence(cfg);
-  return rc != POP_OK ? rc : (recur_workspace_floats(cfg->P, cfg->batch, cfg->T, cfg->C) * 4 + kAlignment - 1) / kAlignment * kAlignment;
+  return rc != POP_OK ? rc : (recur_workspace_floats(cfg->P, cfg->batch, cfg->T, cfg->C, element_bytes(cfg->dtype)) * 4 + kAlignment - 1) / kAlignment * kAlignment;
 }
 
 int64_t pop_recurrence_states_bytes(const pop_recurrence_config* cfg) {
@@ -180,7 +186,7 @@ int pop_recurrence_forward(const pop_recurrence_config* cfg, const pop_recurrenc
                            int64_t workspace_bytes, void* hip_stream) {
   RecurArgs a;
   int rc = recurrence_args(cfg, io, a);
-  if (rc != POP_OK) return rc;
+  if (rc != POP_OK || (rc = check_columns(cfg)) != POP_OK) return rc;
   if (cfg->T > 0) {
     if ((rc = check_sequence(cfg, io->y, "y", true, element_bytes(cfg->dtype))) != POP_OK) return rc;
     if (io->y.data == io->x.data || io->y.data == io->g.data) return fail_thread(POP_EINVAL, "y must not overlap x or g");
@@ -194,7 +200,7 @@ int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurren
                             void* workspace, int64_t workspace_bytes, void* hip_stream) {
   RecurArgs a;
   int rc = recurrence_args(cfg, io, a);
-  if (rc != POP_OK) return rc;
+  if (rc != POP_OK || (rc = check_columns(cfg)) != POP_OK) return rc;
   if (!grads) return fail_thread(POP_EINVAL, "grads is NULL");
   if ((rc = check_floats(grads->dh_last, "dh_last", false)) != POP_OK || (rc = check_floats(grads->dh0, "dh0", false)) != POP_OK ||
       (rc = check_floats(grads->dbias, "dbias", false)) != POP_OK)

@@ -32,7 +32,7 @@ struct RecurArgs {
 };
 
 inline int64_t recur_chunks(int64_t T) { return (T + kRecurChunk - 1) / kRecurChunk; }
-int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C);
+int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C, int64_t element);
 hipError_t launch_recur_forward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_backward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_step(const RecurArgs& a, int dtype, hipStream_t s);

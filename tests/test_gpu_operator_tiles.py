@@ -20,6 +20,61 @@ def test_recurrence_over_many_sequences(shape, dtype):
     _verify(*_case(*shape, dtype=dtype, seed=sum(shape)))
 
 
+# sequences whose tiles are handed from workgroup to workgroup: 64 groups of 64 columns or more in fp32, 128 in 16 bits,
+# up to 256, and in fp32 beyond them from eight tiles on
+CHAINS = [(10, 7, 300, 65, F32), (16, 5, 700, 64, F32), (8, 33, 1100, 64, F32), (9, 15, 400, 64, BF16), (133, 2, 260, 33, F16),
+          (4, 4, 3500, 256, F32), (250, 1, 129, 33, F32)]
+
+
+@pytest.mark.parametrize("P, B, T, C, dtype", CHAINS)
+def test_recurrence_chains(P, B, T, C, dtype):
+    ensure_built()
+    _verify(*_case(P, B, T, C, dtype=dtype, seed=P))
+
+
+@pytest.mark.parametrize("P, B, T, C, dtype", [CHAINS[0], CHAINS[1], CHAINS[3]])
+def test_what_masks_hide_does_not_show_in_chains(P, B, T, C, dtype):
+    ensure_built()
+    kw, dy, dh = _case(P, B, T, C, dtype=dtype, seed=9)
+    kw["lengths"][1, 2], kw["reset"][1, 2, 0] = T, 1
+    kw["h0"][1, 2] = float("nan")                        # in front of a reset
+    behind = torch.arange(T, device="cuda")[None, None] >= kw["lengths"].clamp(0, T)[..., None]
+    kw["x"][behind], kw["g"][behind], dy[behind] = float("nan"), float("inf"), float("nan")
+    kw["reset"][behind] = 1
+    got = _verify(kw, dy, dh)
+    assert all(bool(torch.isfinite(v).all()) for v in got.values())
+
+
+@pytest.mark.parametrize("P, B, T, C, dtype", [CHAINS[0], CHAINS[3]])
+def test_chains_on_streams_and_in_graphs(P, B, T, C, dtype):
+    ensure_built()
+    kw, dy, dh = _case(P, B, T, C, dtype=dtype, seed=10)
+    plan, back = pp.Recurrence(P, B, T, C, dtype), {k: v for k, v in kw.items() if k != "h0"}
+
+    def both():
+        y, h, states = plan.forward(save=True, **kw)
+        return (y, h) + plan.backward(states, dy=dy, dh_last=dh, **back)
+
+    want, side = both(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = both()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    for seed in range(3):
+        new, ndy, _ = _case(P, B, T, C, dtype=dtype, seed=20 + seed)
+        for name in ("x", "g", "bias", "h0", "reset", "lengths"):
+            kw[name].copy_(new[name])
+        dy.copy_(ndy)
+        graph.replay()
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), seed
+
+
 @pytest.mark.parametrize("count, rows, cols, dtype", [(40, 256, 256, F32), (70, 256, 200, F32), (33, 130, 256, F32), (9, 512, 600, F32),
                                                       (70, 140, 256, BF16), (20, 200, 500, F16), (4, 300, 1000, BF16), (1, 700, 1100, BF16),
                                                       (40, 65, 100, F32), (3, 640, 640, F32)])

@@ -188,3 +188,10 @@ def test_muon_refuses(lib):
         assert call(**kw) == pp.POP_EINVAL, kw
     assert call(size=100) == pp.POP_ENOMEM
     assert call(rows=20000) == pp.POP_EUNSUPPORTED
+
+
+def test_more_columns_than_a_grid_takes(lib):
+    cfg, io = _config(P=1 << 14, batch=1 << 14, C=2), _io(states=8 * ADDRESS)
+    assert lib.pop_recurrence_forward(C.byref(cfg), C.byref(io), ADDRESS, 1 << 60, None) == pp.POP_EUNSUPPORTED
+    assert "2^28" in pp.pop_last_error(None)
+    assert lib.pop_recurrence_backward(C.byref(cfg), C.byref(io), C.byref(_grads()), ADDRESS, 1 << 60, None) == pp.POP_EUNSUPPORTED
