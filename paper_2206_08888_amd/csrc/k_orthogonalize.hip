@@ -186,6 +186,8 @@ __device__ inline double block_sum(double v, double* red) {
   return red[0] + red[1] + red[2] + red[3];
 }
 
+// The momentum's step and the sum of U's squares, a part of a matrix per workgroup; bound by memory (80 policies of 17 x 256, 256 x
+// 256 and 256 x 6 in fp32: 14 us for 69 MB).
 template <typename G>
 __global__ void __launch_bounds__(kThreads) k_norms(Args c, Ends ends, char* ws) {
   __shared__ double red[4];
@@ -319,6 +321,8 @@ __device__ inline Corner corner(int matrix, int64_t matrix_stride, int64_t row_s
   return {matrix * matrix_stride + i * row_stride + j, j < cols ? max(rows - i, 0) : 0};
 }
 
+// X = U / (|U| + eps) in blocks of both orders, and the factors of all steps; bound by memory's latency (the same policies: 17 us
+// for 46 MB read, 46 and the padding to whole blocks written).
 template <typename G>
 __global__ void __launch_bounds__(kThreads) k_start(Args c, Bounds bounds, Ends ends, char* ws) {
   __shared__ double red[4];
@@ -524,7 +528,9 @@ __device__ inline void write_block(const f32x4 (&v)[4], _Float16* to, _Float16* 
   __builtin_amdgcn_wave_barrier();
 }
 
-// One 32 x 32 block per workgroup; the wavefronts take a quarter of the contraction each, then a quarter of the block.
+// One 32 x 32 block per workgroup; the wavefronts take a quarter of the contraction each, then a quarter of the block.  Bound
+// by latency (arguments, matrix head, operands, LDS, results: ten of 256 x 256, X X^T 5.3 us, B 5.7, of which 1 is matrix
+// time); a launch's gap is another 1 to 2 us.
 template <int MODE, typename G, typename E>
 __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
   __shared__ float part[4][16][64];
@@ -589,8 +595,8 @@ __global__ void __launch_bounds__(kThreads) k_block(Args c, E ends, char* ws) {
   }
 }
 
-// kMix and kApply: tiles of 64 x 64, a block per wavefront, operands straight from the caches into registers, four blocks of the contraction
-// ahead.
+// kMix and kApply: tiles of 64 x 64, a block per wavefront, operands straight from the caches into registers, four blocks of
+// the contraction ahead.  Bound by latency as k_block, with half of its traffic: ten of 256 x 256, X = Q X 8.1 us.
 constexpr int kQuad = 2;                    // bands of a tile's side
 template <int MODE, typename G, typename E>
 __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
@@ -666,7 +672,10 @@ __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
 // Tiles of 128 x 64 BJ, 64 x 32 BJ per wavefront, 32 contraction indices at a time.  The right operand goes through LDS, the
 // left one, which two wavefronts share, straight into registers.  The next stage is on its way in registers.  With 2048 x
 // 2048 matrices 128 x 128 tiles run at 840 TFLOP/s of fp16 products, prologue and epilogue included, where a large fp16
-// product of the library reaches 1130.
+// product of the library reaches 1130.  Four of 1024 x 4096: X = Q X 127 us, 815 TFLOP/s; X X^T 107, 540, as the triangle's
+// 288 half tiles take two rounds of 256 CUs; squares of A 33, 440, for the same reason.  Products of 256 x 256 (80 of them:
+// X X^T 20, B 18, X 25) are short of stages, eight, beside their prologue and epilogue.  Eight wavefronts with both operands
+// in LDS: the same time; four wavefronts so: 395 against 358 us a step of 80 agents.
 constexpr int kTile = 4, kTileThreads = 256;
 template <int MODE, typename G, typename E, int BJ>
 __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* ws) {
