@@ -672,26 +672,54 @@ __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
 // Tiles of 128 x 64 BJ, 64 x 32 BJ per wavefront, 32 contraction indices at a time.  The right operand goes through LDS, the
 // left one, which two wavefronts share, straight into registers.  The next stage is on its way in registers.  With 2048 x
 // 2048 matrices 128 x 128 tiles run at 840 TFLOP/s of fp16 products, prologue and epilogue included, where a large fp16
-// product of the library reaches 1130.  Four of 1024 x 4096: X = Q X 127 us, 815 TFLOP/s; X X^T 107, 540, as the triangle's
-// 288 half tiles take two rounds of 256 CUs; squares of A 33, 440, for the same reason.  Products of 256 x 256 (80 of them:
+// product of the library reaches 1130.  Four of 1024 x 4096: X = Q X 127 us, 815 TFLOP/s; X X^T 100, 580, and
+// squares of A 31, 470, as 288 half tiles on 256 CUs leave some with two.  Products of 256 x 256 (80 of them:
 // X X^T 20, B 18, X 25) are short of stages, eight, beside their prologue and epilogue.  Eight wavefronts with both operands
 // in LDS: the same time; four wavefronts so: 395 against 358 us a step of 80 agents.
+//
+// Halves of tiles on the diagonal: the left one's lower blocks are the right one's upper blocks mirrored and are not
+// computed.  Such light halves are dealt out last, as those are the workgroups that share a CU with another: four of 1024 x
+// 1024, 256 heavy halves and 32 light ones on 256 CUs: squares 34.2 us with all halves alike, 31.3 so, X X^T over 4096 111 and
+// 100.
 constexpr int kTile = 4, kTileThreads = 256;
+// The task, tile, half (and at.matrix) of a workgroup: an eighth of the heavy halves per XCD, behind them an eighth of the light ones.
+__device__ inline int light_last(const Args& c, At& at, int side, int& ti, int& tj, int& half) {
+  const int tasks = at.l.per / (2 * tiles(side)), light = tasks * side, heavy = at.l.per - light;
+  const int i = (int)blockIdx.x - c.first[at.layer], rank = i >> 3, before = (heavy * at.l.count + 7) / 8;
+  const bool is_heavy = rank < before;
+  const int per = is_heavy ? heavy : light, total = per * at.l.count;
+  const int n = is_heavy ? (i & 7) * before + rank : (i & 7) * ((total + 7) / 8) + rank - before;
+  at.matrix = n < total && (is_heavy || rank - before < (total + 7) / 8) ? n / per : -1;
+  int u = n % per;
+  const int task = u / (per / tasks);
+  u -= task * (per / tasks);
+  if (is_heavy) {
+    ti = 0;
+    while (u >= 2 * (side - ti) - 1) { u -= 2 * (side - ti) - 1; ++ti; }
+    tj = ti + (u + 1) / 2;
+    half = (u + 1) & 1;
+  } else {
+    ti = tj = u;
+    half = 0;
+  }
+  return task;
+}
 template <int MODE, typename G, typename E, int BJ>
 __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* ws) {
   __shared__ __attribute__((aligned(16))) _Float16 staged[2][2 * BJ * 2 * kPair];
   __shared__ __attribute__((aligned(16))) unsigned all_scratch[4][32 * kStride];
   warm_args<sizeof(Args) + (std::is_same<E, Ends>::value ? 256 : 0)>();
-  const At at = find(c);
-  if (at.matrix < 0) return;
+  At at = find(c);
   const Place p = place(at.l.mb, at.l.nb);
-  _Float16* base = halves_of(ws, at, p);
   const int side = (p.mb + kTile - 1) / kTile;
   int unit = BJ == 2 ? at.unit : at.unit >> 1, ti, tj;         // a tile of 128 x 128, and which half of it
-  const int half_of = BJ == 2 ? 0 : at.unit & 1;
+  int half_of = BJ == 2 ? 0 : at.unit & 1;
+  if (BJ == 1 && MODE < kApply) unit = light_last(c, at, side, ti, tj, half_of) * tiles(side);
+  if (at.matrix < 0) return;
+  _Float16* base = halves_of(ws, at, p);
   const Product o = product_of<MODE>(c, at, p, base, unit, side);
   if (MODE < kApply) {
-    triangle(side, unit, ti, tj);
+    if (BJ == 2) triangle(side, unit, ti, tj);
   } else {
     const int jt = (o.jbands + kTile - 1) / kTile;
     ti = unit / jt;
@@ -745,6 +773,14 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
   const StepFactors& step = head_of(ws, at).step[c.step];
   const Factors f = factors_of<MODE>(step, o.q_task), fq = step.q;
   sync_lds();
+  if (BJ == 1 && MODE < kApply && ti == tj && half_of == 0 && __builtin_amdgcn_readfirstlane(wi)) {
+    for (int g = 0; g < (stages & ~1); ++g) {                  // below the diagonal: only the right operand is brought
+      land((g & 1) ^ 1);
+      fetch_right(g + 2);
+      sync_lds();
+    }
+    return;
+  }
   // a stage: its right operand is in LDS half `half`, its left one in `now`; the next ones on their way
   const auto stage_of = [&](int g, int half, const Left& now, Left& next) {
     fetch_left(next, g + 1);
@@ -759,7 +795,7 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
   }
   if (stages & 1) multiply(0, left[0]);
   unsigned* scratch = all_scratch[wave];
-  const bool mirrored = MODE == kApply || (MODE < kApply && ti != tj);
+  const bool mirrored = MODE == kApply || (MODE < kApply && (ti != tj || (BJ == 1 && half_of == 1 && wi == 0)));
 #pragma unroll
   for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
@@ -1072,8 +1108,9 @@ __global__ void __launch_bounds__(kThreads) k_no_steps(Args c, Ends ends, char* 
 
 // ---- launches
 
-// Fills in a launch's workgroups, `per(layer, place)` for each matrix; returns their number.
-template <typename F> int lay_out(const NsCall& c, Args& a, F per) {
+// Fills in a launch's workgroups, `per(layer, place)` for each matrix and `spare` (a multiple of 8) for each layer; returns their
+// number.
+template <typename F> int lay_out(const NsCall& c, Args& a, int spare, F per) {
   int64_t off = 0;
   int blocks = 0;
   for (int k = 0; k < POP_MUON_MAX_LAYERS; ++k) {
@@ -1083,7 +1120,7 @@ template <typename F> int lay_out(const NsCall& c, Args& a, F per) {
     const NsLayer& l = c.layer[k];
     const Place p = place_of(l.rows, l.cols);
     a.layer[k] = {per(l, p), l.count, p.mb, p.nb, off, l.rows > l.cols};
-    blocks += (l.count * a.layer[k].per + 7) / 8 * 8;
+    blocks += (l.count * a.layer[k].per + 7) / 8 * 8 + (a.layer[k].per ? spare : 0);
     off += ns_workspace_bytes(l.count, l.rows, l.cols);
   }
   // a layer without workgroups starts where the next one does, and is passed over
@@ -1100,7 +1137,7 @@ Args args_of(int step, int first, int last, int xt) {
 }
 
 // Which kernel a product takes, by the 128 x 128 tiles of the whole launch (us: k_tile of 128 x 128 / of 128 x 64 / k_quad
-// for kMix and kApply, else k_block).  256 x 256 matrices, X X^T of 8: 11.0 / 7.3 / 4.7, 20: 11.8 / 8.9 / 6.5, 40: 12.7 / 10.0
+// for kMix and kApply, else k_block; light halves as heavy ones).  256 x 256 matrices, X X^T of 8: 11.0 / 7.3 / 4.7, 20: 11.8 / 8.9 / 6.5, 40: 12.7 / 10.0
 // / 9.7, 80: 14.8 / 14.5 / 15.8, 160: 24.3 / 27.0 / 28.5; X = Q X of 20: 13.3 / 10.2 / 12.4, 40: 14.2 / 14.6 / 16.2, 80: 23.0 /
 // 21.5 / 27.6; four of 1024 x 4096: X X^T 108 / 113 / 120, X = Q X 127 / 150 / 223; one of 2048 x 2048: 54 / 58 / 73.
 constexpr int kTilesFrom = 256, kHalvesFrom = 128, kQuadsFrom = 128;
@@ -1108,7 +1145,8 @@ constexpr int kTilesFrom = 256, kHalvesFrom = 128, kQuadsFrom = 128;
 template <int MODE, typename G, typename E, typename N>
 void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
   const auto with = [&](int side, int halves) {
-    return lay_out(c, a, [&](const NsLayer&, const Place& p) { return halves * count(p, (p.mb + side - 1) / side, (p.nb + side - 1) / side); });
+    // (two kinds of halves, each dealt out by eighths)
+    return lay_out(c, a, halves == 2 && MODE < kApply ? 8 : 0, [&](const NsLayer&, const Place& p) { return halves * count(p, (p.mb + side - 1) / side, (p.nb + side - 1) / side); });
   };
   int blocks = with(kTile, 1);
   if (blocks == 0) return;
@@ -1152,11 +1190,11 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     coefs.eps = c.eps;
     for (int k = 0; k < POP_NS_MAX_STEPS; ++k)
       for (int i = 0; i < 3; ++i) coefs.coef[k][i] = c.coef[k][i];
-    blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return pieces(l.rows > l.cols ? l.rows : l.cols); });
+    blocks = lay_out(c, a, 0, [](const NsLayer& l, const Place&) { return pieces(l.rows > l.cols ? l.rows : l.cols); });
     k_gram64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
-    blocks = lay_out(c, a, [](const NsLayer&, const Place&) { return 1; });
+    blocks = lay_out(c, a, 0, [](const NsLayer&, const Place&) { return 1; });
     k_square64<<<dim3(blocks), kSquareThreads, 0, stream>>>(a, ends, coefs, ws);
-    blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return ((l.rows > l.cols ? l.rows : l.cols) + kChunk - 1) / kChunk; });
+    blocks = lay_out(c, a, 0, [](const NsLayer& l, const Place&) { return ((l.rows > l.cols ? l.rows : l.cols) + kChunk - 1) / kChunk; });
     k_last64<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
     return hipGetLastError();
   }
@@ -1170,13 +1208,13 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
     bounds.q_most[k] = c.q_most[k];
   }
   bounds.gain[POP_NS_MAX_STEPS] = c.gain[POP_NS_MAX_STEPS];
-  blocks = lay_out(c, a, [](const NsLayer& l, const Place&) { return parts(l.rows, l.cols); });
+  blocks = lay_out(c, a, 0, [](const NsLayer& l, const Place&) { return parts(l.rows, l.cols); });
   k_norms<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
   if (c.steps == 0) {
     k_no_steps<G><<<dim3(blocks), kThreads, 0, stream>>>(a, ends, ws);
     return hipGetLastError();
   }
-  blocks = lay_out(c, a, [](const NsLayer&, const Place& p) { return (p.mb * p.nb + 3) / 4; });
+  blocks = lay_out(c, a, 0, [](const NsLayer&, const Place& p) { return (p.mb * p.nb + 3) / 4; });
   k_start<G><<<dim3(blocks), kThreads, 0, stream>>>(a, bounds, ends, ws);
   const NoEnds none;
   const auto square = [](const Place&, int m, int) { return tiles(m); };
