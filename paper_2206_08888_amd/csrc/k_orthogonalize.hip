@@ -1140,7 +1140,10 @@ Args args_of(int step, int first, int last, int xt) {
 // for kMix and kApply, else k_block; light halves as heavy ones).  256 x 256 matrices, X X^T of 8: 11.0 / 7.3 / 4.7, 20: 11.8 / 8.9 / 6.5, 40: 12.7 / 10.0
 // / 9.7, 80: 14.8 / 14.5 / 15.8, 160: 24.3 / 27.0 / 28.5; X = Q X of 20: 13.3 / 10.2 / 12.4, 40: 14.2 / 14.6 / 16.2, 80: 23.0 /
 // 21.5 / 27.6; four of 1024 x 4096: X X^T 108 / 113 / 120, X = Q X 127 / 150 / 223; one of 2048 x 2048: 54 / 58 / 73.
-constexpr int kTilesFrom = 256, kHalvesFrom = 128, kQuadsFrom = 128;
+// Triangles, whose light halves come last, keep halves up to 400 tiles (all steps of fp32 calls, 128 x 128 / halves): 272 tiles
+// (two of 2048 x 2048) 1443 / 1304, 288 (eight of 1024 x 1024) 793 / 736, 300 (100 of 256 x 256) 331 / 303, 390 404 / 400, 408
+// (three of 2048 x 2048) 1793 / 1873, 500 (50 of 512 x 512) 771 / 787.
+constexpr int kTilesFrom = 256, kTrianglesFrom = 400, kHalvesFrom = 128, kQuadsFrom = 128;
 
 template <int MODE, typename G, typename E, typename N>
 void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
@@ -1150,7 +1153,7 @@ void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_
   };
   int blocks = with(kTile, 1);
   if (blocks == 0) return;
-  if (blocks >= kTilesFrom) {
+  if (blocks >= (MODE < kApply ? kTrianglesFrom : kTilesFrom)) {
     k_tile<MODE, G, E, 2><<<dim3(blocks), kTileThreads, 0, stream>>>(a, ends, ws);
     return;
   }

@@ -117,3 +117,16 @@ def test_muon_steps_of_many_agents(P, shapes, dtype, nesterov):
     scales = [float(np.float32(max(1.0, r / c) ** 0.5)) for r, c in shapes]
     plan = pp.Muon(P, shapes, dtype=dtype, scales=scales, nesterov=nesterov)
     _check_muon(plan, *_muon_case(P, shapes, dtype, 31), nesterov, scales)
+
+
+@pytest.mark.parametrize("count, rows, cols, dtype", [(100, 256, 256, F32), (30, 512, 400, F32), (34, 400, 640, BF16), (150, 200, 256, F16)])
+def test_halves_and_whole_tiles_of_triangles(count, rows, cols, dtype):
+    """From 128 to 400 tiles, and beyond: a matrix's result goes by its tiling alone within rounding."""
+    ensure_built()
+    g = _gradient((count, rows, cols), dtype, 5)
+    o = pp.Orthogonalizer(count, rows, cols, dtype)(g)
+    for p in (0, count // 2, count - 1):
+        _check(o[p:p + 1], g[p:p + 1], QUINTIC, 1e-7, dtype)
+    few = pp.Orthogonalizer(2, rows, cols, dtype)(g[:2])
+    _check(few, g[:2], QUINTIC, 1e-7, dtype)
+    assert bool(torch.isfinite(o).all())
