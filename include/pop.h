@@ -386,7 +386,7 @@ typedef struct {
   pop_sequence dy;        /* gradient of y */
   pop_sequence dx, dg;    /* written */
   const float* dh_last;   /* [P, batch, C] gradient of h_last, or NULL: zeros */
-  float* dh0;             /* written: [P, batch, C], or NULL */
+  float* dh0;             /* written: [P, batch, C], or NULL; may be dh_last */
   float* dbias;           /* written: [P, C], summed over sequences and steps in a fixed order, or NULL */
 } pop_recurrence_grads;
 

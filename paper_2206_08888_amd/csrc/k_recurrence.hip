@@ -160,6 +160,11 @@ __global__ void __launch_bounds__(kThreads) k_clear(unsigned long long* words, i
   if (i < n) words[i] = 0;
 }
 
+// h0 (backward: dh_last) as the launch of maps found it, behind maps and sums: the last segment of kSegments writes
+// h_last, which may lie over h0, while other segments have yet to start.  (kWhole reads and writes a column in one
+// lane; in kChain only the first tile reads h0, and what the last one writes has passed through all of them.)
+__device__ inline float* first_of(const RecurArgs& a, int64_t n, int segments) { return a.ws + 3 * n * segments + 2; }
+
 // This workgroup's columns and tiles.
 struct Place { int64_t first; int seg, segments; };
 template <int MODE> __device__ inline Place place_of(const RecurArgs& a, int64_t n, int segments, bool backward) {
@@ -237,8 +242,10 @@ __global__ void __launch_bounds__(8192 / N) k_forward(RecurArgs a, int chunks, i
   const int64_t column = place.first + (threadIdx.x & 63);
   const bool carries = threadIdx.x < kColumns && column < n;
   float carry = 0.0f, A_all = 1.0f;
-  if (MODE != kMaps) {
-    if (a.h0 && column < n && (MODE != kChain || place.seg == 0)) carry = a.h0[column];
+  if (MODE == kMaps) {
+    if (a.h0 && carries && place.seg == 0) first_of(a, n, segments)[column] = a.h0[column];
+  } else {
+    if (a.h0 && column < n && (MODE != kChain || place.seg == 0)) carry = MODE == kSegments ? first_of(a, n, segments)[column] : a.h0[column];
     if (MODE == kSegments) carry = enter(a, n, column, segments, 0, place.seg, 1, carry, quarter);
   }
 
@@ -407,6 +414,7 @@ __global__ void __launch_bounds__(8192 / N) k_backward_maps(RecurArgs a, int chu
     }
   }
   if (threadIdx.x < kColumns && column < n) {
+    if (a.dh_last && (int)blockIdx.y == segments - 1) first_of(a, n, segments)[column] = a.dh_last[column];
     float* to = a.ws + (int64_t)blockIdx.y * n + column;
     to[0] = A_all;
     to[(int64_t)segments * n] = d;
@@ -445,7 +453,8 @@ __global__ void __launch_bounds__(8192 / N, 2) k_backward(RecurArgs a, int chunk
   // a column per lane: wavefront 0 carries the gradient from tile to tile, wavefront 1 takes states from `states`
   const int64_t column = place.first + lane, row = column / a.C;
   const bool valid = column < n;
-  float d = a.dh_last && valid && (MODE != kChain || k1 == chunks) ? a.dh_last[column] : 0.0f;
+  float d = 0.0f;
+  if (a.dh_last && valid && (MODE != kChain || k1 == chunks)) d = MODE == kSegments ? first_of(a, n, segments)[column] : a.dh_last[column];
   if (MODE == kSegments) d = enter(a, n, column, segments, segments - 1, segments - 1 - place.seg, -1, d, quarter);
   const float* states = a.states + row * chunks * a.C + (column - row * a.C);
   const int64_t dx_at = base(a.dx, l) + l.c, dg_at = base(a.dg, l) + l.c;
@@ -763,7 +772,9 @@ template <typename E> hipError_t step(const RecurArgs& a, hipStream_t s) {
 }  // namespace
 
 int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C, int64_t element) {
-  return T == 0 ? 0 : 3 * P * B * C * recur::cut_of(P, B, T, C, element).segments + 2;   // maps or words (and the ticket), sums
+  if (T == 0) return 0;
+  const recur::Cut c = recur::cut_of(P, B, T, C, element);
+  return P * B * C * (3 * c.segments + (c.mode == recur::kSegments)) + 2;      // maps or words (and the ticket), sums, first states
 }
 
 hipError_t launch_recur_forward(const RecurArgs& a, int dtype, hipStream_t s) {
