@@ -12,7 +12,11 @@
 // 64 bits, segments of 1 / 2 / 3 steps, over those of fp32 products: 0.78 / 1.6 / 2.6 in the mean of 40 shapes, 3 / 8 / 66 at
 // most (small square matrices, one of whose singular values is small).  So results in fp32 take one step per segment,
 // and results of 16 bits, whose rounding is 2e-4 or more, three where that is less work, from n = 1.5 m on (four 1024 x
-// 4096: 877 us, with one step 1286; 256 x 256: 114, with one 102).
+// 4096: 877 us, with one step 1286; 256 x 256: 114, with one 102).  Steep steps enlarge the difference: errors of A, 2^-22 of
+// its largest entries, are multiplied by what a step multiplies A by, the square of its slope at 0 and about.  Segments of
+// three are taken while all steps together multiply A by at most 2^22 (kSegmentGain squared; five and six steps of the usual
+// quintic: 2^17.8 and 2^21.4); eight of slope 5, 2^37, had up to 16 times the error of fp32 products, with one step less than
+// theirs.
 //
 // All matrices of a call advance together, a launch per product.  Calls whose matrices all have m up to 64 take a path of
 // their own: the squares of A, Q and so on fit a workgroup, and with everything in 64 bits all steps are one segment (below,

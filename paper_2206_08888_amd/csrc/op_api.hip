@@ -96,7 +96,8 @@ void bounds_of(const pop_ns_config& c, NsCall& n) {
   n.gain[c.steps] = (float)fmin(gain, 1e30);
 }
 
-int check_ns(const pop_ns_config* c, int32_t dtype, int segment, NsCall& n) {
+// three: whether the results' type and the matrices' shape allow segments of three steps (k_orthogonalize.hip has the reasons)
+int check_ns(const pop_ns_config* c, int32_t dtype, bool three, NsCall& n) {
   if (!c) return fail_thread(POP_EINVAL, "config is NULL");
   if (c->steps < 0 || c->steps > POP_NS_MAX_STEPS) return fail_thread(POP_EINVAL, "steps must be 0 .. %d", (int)POP_NS_MAX_STEPS);
   if (!(c->eps >= 1e-30f && c->eps <= 1e30f)) return fail_thread(POP_EINVAL, "eps must be within 1e-30 .. 1e30");
@@ -105,8 +106,12 @@ int check_ns(const pop_ns_config* c, int32_t dtype, int segment, NsCall& n) {
     for (float v : c->coef[k])
       if (!isfinite(v)) return fail_thread(POP_EINVAL, "coefficients of step %d are not finite", k);
   n = NsCall{};
-  n.segment = segment;
+  n.segment = 1;
   bounds_of(*c, n);
+  if (three && n.gain[c->steps] <= kSegmentGain) {
+    n.segment = 3;
+    bounds_of(*c, n);
+  }
   if (!(n.most <= kMostSingular)) return fail_thread(POP_EUNSUPPORTED, "the coefficients let singular values of at most 1 grow beyond %g", kMostSingular);
   n.steps = c->steps;
   n.eps = c->eps;
@@ -245,9 +250,8 @@ int64_t pop_orthogonalize_workspace_bytes(int32_t count, int32_t rows, int32_t c
 int pop_orthogonalize(const pop_ns_config* cfg, int32_t count, int32_t rows, int32_t cols, int32_t dtype, const pop_matrices* g,
                       const pop_matrices* out, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   NsCall n;
-  // (the rule's reasons: k_orthogonalize.hip)
   const int64_t side = rows < cols ? rows : cols, other = rows < cols ? cols : rows;
-  int rc = check_ns(cfg, dtype, dtype != POP_F32 && 2 * other >= 3 * side ? 3 : 1, n);
+  int rc = check_ns(cfg, dtype, dtype != POP_F32 && 2 * other >= 3 * side, n);
   if (rc != POP_OK || (rc = check_shape(count, rows, cols)) != POP_OK) return rc;
   if (!g || !out) return fail_thread(POP_EINVAL, "g or out is NULL");
   if ((rc = check_matrices(count, rows, cols, *g, "g", false, element_bytes(dtype))) != POP_OK ||
@@ -269,7 +273,7 @@ int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_lay
 int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype, int32_t nesterov,
                   const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes, void* hip_stream) {
   NsCall n;
-  int rc = check_ns(cfg, dtype, 1, n);
+  int rc = check_ns(cfg, dtype, false, n);
   if (rc != POP_OK) return rc;
   const int64_t need = muon_workspace(P, n_layers, layers);
   if (need < 0) return (int)need;

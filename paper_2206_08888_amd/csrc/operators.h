@@ -41,6 +41,7 @@ hipError_t launch_recur_step(const RecurArgs& a, int dtype, hipStream_t s);
 // ---- orthogonalised updates
 
 constexpr int kNsMaxSide = 16384;
+constexpr float kSegmentGain = 0x1p11f;    // most that all steps together may multiply small singular values by for segments of three
 
 struct NsLayer {                     // matrices of one shape
   int rows, cols, count;
