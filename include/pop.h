@@ -416,7 +416,8 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  *
  * which drives the singular values of G towards 1.  All sums are fp32 (|G|: fp64).  Products run on the fp16 matrix
  * instructions from operands split into two halves of 11 bits each, which is fp32's precision up to the last bits; calls
- * whose matrices all have at most 64 rows or columns run in fp64. */
+ * whose matrices all have at most 64 rows or columns run in fp64, unless the steps together multiply small singular values by
+ * more than 2^20 (five steps of 3.4445, -4.775, 2.0315: 2^8.9). */
 enum { POP_NS_MAX_STEPS = 16 };
 typedef struct {
   int32_t steps;                        /* 0 .. POP_NS_MAX_STEPS */

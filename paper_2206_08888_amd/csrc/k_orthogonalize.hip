@@ -19,8 +19,8 @@
 // theirs.
 //
 // All matrices of a call advance together, a launch per product.  Calls whose matrices all have m up to 64 take a path of
-// their own: the squares of A, Q and so on fit a workgroup, and with everything in 64 bits all steps are one segment (below,
-// k_gram64).  (Beside larger matrices small ones cost nothing, and launches of their own would.)
+// their own: the squares of A, Q and so on fit a workgroup, and with everything in 64 bits all steps are one segment, unless they
+// are too many or too steep (below, k_gram64).  (Beside larger matrices small ones cost nothing, and launches of their own would.)
 //
 // Products on v_mfma_f32_32x32x16_f16 from operands in two fp16 halves, x = hi + lo with 11 bits each, held in units
 // (powers of two, Units below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
@@ -47,6 +47,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPair = 1024;                 // halves of a hi and a lo block
 constexpr int kSmall = 2;                   // bands of m up to which matrices can take the path in 64 bits
+constexpr float kSmallGain = 0x1p20f;       // most that all steps together may multiply small singular values by there
 
 // Where the arrays of one matrix lie, in halves from the start of its workspace.
 struct Place {
@@ -839,11 +840,16 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
 // ---- m <= 64, in 64 bits
 
 // The 64-bit path: k_gram64 updates the momentum and sums U U^T over a piece of n, k_square64 adds the pieces up (the trace
-// is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Errors: the rounding
-// of the result.  Three launches, in which k_square64's products, one after the other in one workgroup per matrix, are the
-// longest part: 8 of 17 x 2000 30 us (48 as fp16 halves in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58).
-// That part on vector instructions made it 119, on the matrix ones with a wavefront's tiles one by one 159, its chains
-// interleaved 92, from eight wavefronts 77.
+// is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Three launches, in which k_square64's
+// products, one after the other in one workgroup per matrix, are the longest part: 8 of 17 x 2000 30 us (48 as fp16 halves
+// in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58).  That part on vector instructions made it 119, on the
+// matrix ones with a wavefront's tiles one by one 159, its chains interleaved 92, from eight wavefronts 77.
+//
+// What rounding makes of an eigenvalue of zero, about 2^-53 of either sign, grows with every step as small eigenvalues do.
+// Large, it is an error of its size; far below zero, steps diverge.  So the path is taken while all steps together multiply
+// eigenvalues by at most 2^40 (kSmallGain squared; eleven steps of the usual quintic: 2^39.3), which leaves 2^-13 of the largest.
+// Up to there errors are the result's rounding or little more (6 x 256 of rank 3, eleven steps: 4e-8, products in 32 bits 1e-2);
+// beyond it, in emulation, 14 steps 8e-3, 16 steps 5.  More or steeper steps take the general path.
 
 constexpr int kChunk = 64, kChunkStride = 65;
 // U's columns (of X) j0 .. j0 + 63 to LDS, zeros outside; `update`: with the momentum's step.
@@ -971,7 +977,9 @@ __global__ void __launch_bounds__(kSquareThreads) k_square64(Args c, Ends ends, 
   }
   __syncthreads();
   // A product of two of the (symmetric) squares, tile by tile: f * left * right + g * old, in both triangles of `to`, which may
-  // be `old` or an operand (behind the barrier all have read it).  A wavefront's tiles take turns, so that no
+  // be `old` or an operand (behind the barrier all have read it).  Elements above the diagonal stand for those below it on
+  // the diagonal's tiles too: what makes A and Q unsymmetric grows by a step's slope to the third, not to the second (with those
+  // tiles as they are computed, 6 x 256 of rank 3, nine steps 2e-4, eleven 0.3).  A wavefront's tiles take turns, so that no
   // instruction waits for the one before it, with the operands of 16 indices read ahead of them.
   struct Task { const double *left, *right, *old; double *to, f, g; };
   const auto phase = [&](const Tiles& mine, const Task (&task)[kMine]) {
@@ -1014,8 +1022,9 @@ __global__ void __launch_bounds__(kSquareThreads) k_square64(Args c, Ends ends, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int i = 16 * mine.i[t] + 4 * r + (lane >> 4), j = 16 * mine.j[t] + (lane & 15);
+          if (i > j) continue;
           task[t].to[element(i, j)] = v[t][r];
-          if (mine.i[t] != mine.j[t]) task[t].to[element(j, i)] = v[t][r];
+          task[t].to[element(j, i)] = v[t][r];
         }
     __syncthreads();
   };
@@ -1191,6 +1200,7 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
   int blocks;
   bool small = true;
   for (int k = 0; k < c.n_layers; ++k) small = small && place_of(c.layer[k].rows, c.layer[k].cols).mb <= kSmall;
+  small = small && c.gain[c.steps] <= kSmallGain;
   if (small) {
     Coefs coefs;
     coefs.steps = c.steps;

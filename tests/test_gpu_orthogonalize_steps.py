@@ -47,3 +47,15 @@ def test_steep_steps_for_16_bit_results(rows, cols, rank, steps, dtype):
     ensure_built()
     err, err32, norm, _ = _errors(_low_rank(rows, cols, rank, dtype), STEEP, steps)
     assert err <= 4 * err32 + ROUNDING[dtype] * norm, (err, err32, norm)
+
+
+@pytest.mark.parametrize("coef, steps", [(pp.NS_COEF, 6), (pp.NS_COEF, 11), (pp.NS_COEF, 12), (pp.NS_COEF, 14), (pp.NS_COEF, 16), (STEEP, 8), (STEEP, 9),
+                                         (STEEP, 12), (STEEP, 14), (STEEP, 16)])
+@pytest.mark.parametrize("rows, cols, rank, dtype", [(6, 256, 3, F32), (17, 256, 8, F32), (50, 64, 10, F32), (64, 300, 40, F32), (300, 40, 20, F32), (64, 64, 64, F32),
+                                                     (300, 40, 20, BF16), (50, 64, 10, F16)])
+def test_many_steps_of_small_deficient_matrices(rows, cols, rank, dtype, coef, steps):
+    """Up to 64 rows or columns, singular values of zero: what rounding makes of those grows with every step."""
+    ensure_built()
+    err, err32, norm, got = _errors(_low_rank(rows, cols, rank, dtype), coef, steps)
+    assert np.isfinite(got).all()
+    assert err <= 4 * err32 + ROUNDING[dtype] * norm, (err, err32, norm)
