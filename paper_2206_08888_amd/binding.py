@@ -48,6 +48,59 @@ class pop_config(C.Structure):
 assert C.sizeof(pop_hparams) == 64 and C.sizeof(pop_config) == 80
 
 
+# ---- operators (their calls on tensors: operators.py)
+
+POP_F32, POP_BF16, POP_F16 = 0, 1, 2
+
+
+class pop_recurrence_config(C.Structure):
+    _fields_ = [("P", C.c_int32), ("batch", C.c_int32), ("T", C.c_int32), ("C", C.c_int32), ("dtype", C.c_int32),
+                ("reserved_", C.c_int32)]
+
+
+class pop_sequence(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("agent", C.c_int64), ("row", C.c_int64), ("step", C.c_int64)]
+
+
+class pop_recurrence_io(C.Structure):
+    _fields_ = [("x", pop_sequence), ("g", pop_sequence), ("y", pop_sequence), ("reset", pop_sequence),
+                ("bias", C.c_void_p), ("h0", C.c_void_p), ("h_last", C.c_void_p), ("lengths", C.c_void_p),
+                ("states", C.c_void_p)]
+
+
+class pop_recurrence_grads(C.Structure):
+    _fields_ = [("dy", pop_sequence), ("dx", pop_sequence), ("dg", pop_sequence), ("dh_last", C.c_void_p),
+                ("dh0", C.c_void_p), ("dbias", C.c_void_p)]
+
+
+NS_MAX_STEPS, MUON_MAX_LAYERS = 16, 8
+NS_COEF = (3.4445, -4.7750, 2.0315)                      # five steps take singular values of 0.01 .. 1 to 0.7 .. 1.2
+
+
+class pop_ns_config(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("eps", C.c_float), ("coef", (C.c_float * 3) * NS_MAX_STEPS)]
+
+
+class pop_matrices(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("matrix", C.c_int64), ("row", C.c_int64)]
+
+
+class pop_muon_layer(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("scale", C.c_float), ("reserved_", C.c_int32),
+                ("grad", pop_matrices), ("momentum", pop_matrices), ("weight", pop_matrices)]
+
+
+def make_ns_config(steps=5, coef=NS_COEF, eps=1e-7):
+    """coef: (k0, k1, k2) for all steps, or one such triple per step."""
+    cfg = pop_ns_config(steps, eps)
+    each = [coef] * steps if not coef or not hasattr(coef[0], "__len__") else list(coef)
+    if len(each) != steps or any(len(k) != 3 for k in each):
+        raise ValueError("coef must be three numbers, or three for each of %d steps" % steps)
+    for k in range(min(steps, NS_MAX_STEPS)):
+        cfg.coef[k][:] = each[k]
+    return cfg
+
+
 class PopError(RuntimeError):
     def __init__(self, code, message):
         super().__init__("pop error %d: %s" % (code, message))

@@ -9,58 +9,13 @@ import ctypes as ct
 
 import torch
 
-from .binding import _check, load_library
+from .binding import (  # noqa: F401
+    MUON_MAX_LAYERS, NS_COEF, NS_MAX_STEPS, POP_BF16, POP_F16, POP_F32, _check, load_library, make_ns_config, pop_matrices,
+    pop_muon_layer, pop_ns_config,
+    pop_recurrence_config, pop_recurrence_grads, pop_recurrence_io, pop_sequence,
+)
 
-POP_F32, POP_BF16, POP_F16 = 0, 1, 2
 DTYPE_CODES = {torch.float32: POP_F32, torch.bfloat16: POP_BF16, torch.float16: POP_F16}
-
-
-class pop_recurrence_config(ct.Structure):
-    _fields_ = [("P", ct.c_int32), ("batch", ct.c_int32), ("T", ct.c_int32), ("C", ct.c_int32), ("dtype", ct.c_int32),
-                ("reserved_", ct.c_int32)]
-
-
-class pop_sequence(ct.Structure):
-    _fields_ = [("data", ct.c_void_p), ("agent", ct.c_int64), ("row", ct.c_int64), ("step", ct.c_int64)]
-
-
-class pop_recurrence_io(ct.Structure):
-    _fields_ = [("x", pop_sequence), ("g", pop_sequence), ("y", pop_sequence), ("reset", pop_sequence),
-                ("bias", ct.c_void_p), ("h0", ct.c_void_p), ("h_last", ct.c_void_p), ("lengths", ct.c_void_p),
-                ("states", ct.c_void_p)]
-
-
-class pop_recurrence_grads(ct.Structure):
-    _fields_ = [("dy", pop_sequence), ("dx", pop_sequence), ("dg", pop_sequence), ("dh_last", ct.c_void_p),
-                ("dh0", ct.c_void_p), ("dbias", ct.c_void_p)]
-
-
-NS_MAX_STEPS, MUON_MAX_LAYERS = 16, 8
-NS_COEF = (3.4445, -4.7750, 2.0315)                      # five steps take singular values of 0.01 .. 1 to 0.7 .. 1.2
-
-
-class pop_ns_config(ct.Structure):
-    _fields_ = [("steps", ct.c_int32), ("eps", ct.c_float), ("coef", (ct.c_float * 3) * NS_MAX_STEPS)]
-
-
-class pop_matrices(ct.Structure):
-    _fields_ = [("data", ct.c_void_p), ("matrix", ct.c_int64), ("row", ct.c_int64)]
-
-
-class pop_muon_layer(ct.Structure):
-    _fields_ = [("rows", ct.c_int32), ("cols", ct.c_int32), ("scale", ct.c_float), ("reserved_", ct.c_int32),
-                ("grad", pop_matrices), ("momentum", pop_matrices), ("weight", pop_matrices)]
-
-
-def make_ns_config(steps=5, coef=NS_COEF, eps=1e-7):
-    """coef: (k0, k1, k2) for all steps, or one such triple per step."""
-    cfg = pop_ns_config(steps, eps)
-    each = [coef] * steps if not coef or not hasattr(coef[0], "__len__") else list(coef)
-    if len(each) != steps or any(len(k) != 3 for k in each):
-        raise ValueError("coef must be three numbers, or three for each of %d steps" % steps)
-    for k in range(min(steps, NS_MAX_STEPS)):
-        cfg.coef[k][:] = each[k]
-    return cfg
 
 
 def _dtype_code(dtype):
@@ -69,7 +24,8 @@ def _dtype_code(dtype):
     return DTYPE_CODES[dtype]
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream         # current_stream(index).cuda_stream without the object around it
+# current_stream(index).cuda_stream, where PyTorch has it without the object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class _Operator:
