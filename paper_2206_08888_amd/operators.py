@@ -4,10 +4,15 @@ HIP kernels of libpop.so, on PyTorch's current stream, asynchronously.
 
 Outputs and workspaces come from PyTorch's allocator, call by call, so calls may run on any stream and inside
 torch.cuda.graph; tensors used on another stream than their own need the usual events and record_stream.
+
+Autograd records none of this: backward passes are calls of their own.  Inputs that require gradients are refused while
+gradients are recorded (pass them detached, or under torch.no_grad()); Muon, as optimisers do, updates weights outside of any
+graph.  Tensors that are written in place raise their version, so that graphs which kept them notice.
 """
 import ctypes as ct
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .binding import (  # noqa: F401
     MUON_MAX_LAYERS, NS_COEF, NS_MAX_STEPS, POP_BF16, POP_F16, POP_F32, _check, load_library, make_ns_config, pop_matrices,
@@ -32,6 +37,8 @@ class _Operator:
     """Device and type checks, and the stream of a call.  Calls are short beside their launches, so the checks take the
     shortest way through what is right and find out what is wrong afterwards."""
 
+    outside_graphs = False                               # whether tensors may require gradients
+
     def __init__(self, dtype, device):
         self.dtype, self.code = dtype, _dtype_code(dtype)
         self.device = torch.device(device)
@@ -45,7 +52,8 @@ class _Operator:
     def _tensor(self, t, name, shape, dtype=None, contiguous=True):
         dtype = dtype or self.dtype
         try:
-            if t.shape == shape and t.dtype is dtype and t.get_device() == self.index and (not contiguous or t.is_contiguous()):
+            if (t.shape == shape and t.dtype is dtype and t.get_device() == self.index and (not contiguous or t.is_contiguous())
+                    and (not t.requires_grad or self.outside_graphs or not torch.is_grad_enabled())):
                 return t
         except AttributeError:
             pass
@@ -55,7 +63,9 @@ class _Operator:
             raise ValueError("%s must be of type %s, not %s" % (name, dtype, t.dtype))
         if t.shape != shape:
             raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-        raise ValueError("%s must be contiguous" % name)
+        if contiguous and not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        raise ValueError("%s requires gradients, which are not recorded here: pass it detached or under torch.no_grad()" % name)
 
     def _pointer(self, t, name, shape, dtype=torch.float32):
         return None if t is None else self._tensor(t, name, shape, dtype).data_ptr()
@@ -161,6 +171,7 @@ class Recurrence(_Operator):
                                self._pointer(bias, "bias", self._channels))
         self._call(self.lib.pop_recurrence_step, self._one_ref, ct.byref(io), self._pointer(state, "state", (self.P, n_slots, self.C)),
                    n_slots, self._pointer(slots, "slots", shape[:2], torch.int32))
+        increment_version(state)
         return y
 
 
@@ -185,11 +196,13 @@ class Orthogonalizer(_NewtonSchulz):
 
     def __call__(self, g, out=None):
         """A new tensor, or `out` (which may be g)."""
-        out = self._empty(self.shape) if out is None else out
+        given, out = out, self._empty(self.shape) if out is None else out
         gm, om = self._matrices(g, "g", self.shape), self._matrices(out, "out", self.shape)
         ws = self._empty(self._bytes, torch.uint8)
         self._call(self.lib.pop_orthogonalize, ct.byref(self._ns), *self.shape, self.code, ct.byref(gm), ct.byref(om),
                    ws.data_ptr(), self._bytes)
+        if given is not None:
+            increment_version(given)
         return out
 
 
@@ -201,6 +214,8 @@ class Muon(_NewtonSchulz):
     Weights and momenta are float32, gradients of `dtype`; any strides with adjacent columns.  shapes: (rows, cols) of
     each layer (at most 8); scales: a factor of each layer's update, by default sqrt(max(1, cols / rows)) (weights are
     [in, out])."""
+
+    outside_graphs = True
 
     def __init__(self, P, shapes, dtype=torch.float32, device="cuda", scales=None, nesterov=True, steps=5, coef=NS_COEF, eps=1e-7):
         super().__init__(dtype, device)
@@ -227,3 +242,4 @@ class Muon(_NewtonSchulz):
         ws = self._empty(self._bytes, torch.uint8)
         self._call(self.lib.pop_muon_step, ct.byref(self._ns), self.P, len(self.shapes), layers, self.code, int(self.nesterov),
                    self._pointer(hparams, "hparams", (self.P, 3)), ws.data_ptr(), self._bytes)
+        increment_version([*weights, *momenta])
