@@ -364,7 +364,7 @@ typedef struct {
 } pop_recurrence_config;
 
 /* A [P, batch, T, C] array: channels adjacent, the other axes with strides in elements (zero: the axis is broadcast,
- * for inputs only; outputs must not overlap themselves or any input). */
+ * for inputs only; outputs must not overlap themselves, each other, any input or the workspace: POP_EINVAL). */
 typedef struct {
   void* data;
   int64_t agent, row, step;
@@ -405,8 +405,8 @@ int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurren
 /* One step for acting agents: x, g, y are [P, batch, C] (cfg->T is 1, the step strides are ignored, reset is [P,
  * batch]), the states live in state[P, n_slots, C] and are updated in place.  slots[P, batch] names the state row of
  * each row, NULL: row b uses slot b.  A row whose slot is negative or not below n_slots is idle: its y is 0, and
- * nothing of it is read.  No two rows of an agent may name the same slot.  io->h0, h_last, lengths and states must
- * be NULL. */
+ * nothing of it is read.  No two rows of an agent may name the same slot.  y may be x or g (with the same strides).
+ * io->h0, h_last, lengths and states must be NULL. */
 int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
                         float* state, int32_t n_slots, const int32_t* slots, void* hip_stream);
 
@@ -459,7 +459,8 @@ enum { POP_MUON_MAX_LAYERS = 8 };
 int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_layer* layers);
 
 /* One optimiser step of every matrix of every agent (the Muon optimiser):
- *   M = mu M + G;   U = nesterov ? G + mu M : M;   W = (1 - lr wd) W - lr scale O,   O = U orthogonalised. */
+ *   M = mu M + G;   U = nesterov ? G + mu M : M;   W = (1 - lr wd) W - lr scale O,   O = U orthogonalised.
+ * Momenta and weights of all layers must not overlap each other or anything else. */
 int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype,
                   int32_t nesterov, const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes,
                   void* hip_stream);

@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdint.h>
 #include "operators.h"
+#include "regions.h"
 
 namespace pop {
 namespace op {
@@ -69,6 +70,21 @@ int check_workspace(void* p, int64_t have, int64_t need) {
   if ((uintptr_t)p % kAlignment) return fail_thread(POP_EINVAL, "workspace must be 256-byte aligned");
   if (have < need) return fail_thread(POP_ENOMEM, "workspace has %lld bytes, %lld needed", (long long)have, (long long)need);
   return POP_OK;
+}
+
+int check_apart(const Regions& r) {
+  const char *one, *other;
+  return r.clash(one, other) ? fail_thread(POP_EINVAL, "%s and %s overlap", one, other) : POP_OK;
+}
+
+void add_sequence(Regions& r, const pop_recurrence_config* c, const pop_sequence& s, const char* name, int64_t bytes, int64_t inner, bool written, int same = 0) {
+  const int64_t n[3] = {c->P, c->batch, c->T}, stride[3] = {s.agent * bytes, s.row * bytes, s.step * bytes};
+  r.add(name, s.data, inner * bytes, 3, n, stride, written, same);
+}
+
+void add_matrices(Regions& r, int64_t count, int64_t rows, int64_t cols, const pop_matrices& m, const char* name, int64_t bytes, bool written, int same = 0) {
+  const int64_t n[2] = {count, rows}, stride[2] = {m.matrix * bytes, m.row * bytes};
+  r.add(name, m.data, cols * bytes, 2, n, stride, written, same);
 }
 
 // NsCall::most, gain and q_most (segment is set).  p(s) = k0 s + k1 s^3 + k2 s^5 is largest at an end of the interval or where p' = 0, a quadratic
@@ -169,6 +185,23 @@ int recurrence_args(const pop_recurrence_config* c, const pop_recurrence_io* io,
   return POP_OK;
 }
 
+// The arrays of all three calls that only a direction of time reads, and those of x, g, y that this call has (y may be x or g in
+// single steps: `same`).
+Regions recurrence_regions(const pop_recurrence_config* c, const pop_recurrence_io* io, bool y, int same = 0) {
+  Regions r;
+  const int64_t e = element_bytes(c->dtype), rows = (int64_t)c->P * c->batch;
+  if (c->T > 0) {
+    add_sequence(r, c, io->x, "x", e, c->C, false, same);
+    add_sequence(r, c, io->g, "g", e, c->C, false, same);
+    if (y) add_sequence(r, c, io->y, "y", e, c->C, true, same);
+    add_sequence(r, c, io->reset, "reset", 1, 1, false);
+  }
+  r.add("bias", io->bias, (int64_t)c->P * c->C * 4, false);
+  r.add("lengths", io->lengths, rows * 4, false);
+  return r;
+}
+enum { kStep = 1, kFirstAndLast = 2 };       // Region::same
+
 }  // namespace op
 }  // namespace pop
 
@@ -194,9 +227,15 @@ int pop_recurrence_forward(const pop_recurrence_config* cfg, const pop_recurrenc
   if (rc != POP_OK || (rc = check_columns(cfg)) != POP_OK) return rc;
   if (cfg->T > 0) {
     if ((rc = check_sequence(cfg, io->y, "y", true, element_bytes(cfg->dtype))) != POP_OK) return rc;
-    if (io->y.data == io->x.data || io->y.data == io->g.data) return fail_thread(POP_EINVAL, "y must not overlap x or g");
   }
-  if ((rc = check_workspace(workspace, workspace_bytes, pop_recurrence_workspace_bytes(cfg))) != POP_OK) return rc;
+  const int64_t need = pop_recurrence_workspace_bytes(cfg), rows = (int64_t)cfg->P * cfg->batch * cfg->C * 4;
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  Regions r = recurrence_regions(cfg, io, true);
+  r.add("h0", io->h0, rows, false, kFirstAndLast);
+  r.add("h_last", io->h_last, rows, true, kFirstAndLast);
+  r.add("states", io->states, rows * recur_chunks(cfg->T), true);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
   a.ws = (float*)workspace;
   return launched(launch_recur_forward(a, cfg->dtype, (hipStream_t)hip_stream));
 }
@@ -215,12 +254,22 @@ int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurren
     if ((rc = check_floats(io->states, "states", true)) != POP_OK || (rc = check_sequence(cfg, grads->dy, "dy", false, e)) != POP_OK ||
         (rc = check_sequence(cfg, grads->dx, "dx", true, e)) != POP_OK || (rc = check_sequence(cfg, grads->dg, "dg", true, e)) != POP_OK)
       return rc;
-    const void* outs[2] = {grads->dx.data, grads->dg.data};
-    for (const void* o : outs)
-      if (o == io->x.data || o == io->g.data || o == grads->dy.data) return fail_thread(POP_EINVAL, "dx and dg must not overlap x, g or dy");
-    if (outs[0] == outs[1]) return fail_thread(POP_EINVAL, "dx and dg must not overlap");
   }
-  if ((rc = check_workspace(workspace, workspace_bytes, pop_recurrence_workspace_bytes(cfg))) != POP_OK) return rc;
+  const int64_t need = pop_recurrence_workspace_bytes(cfg), rows = (int64_t)cfg->P * cfg->batch * cfg->C * 4;
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  Regions r = recurrence_regions(cfg, io, false);
+  if (cfg->T > 0) {
+    const int64_t e = element_bytes(cfg->dtype);
+    add_sequence(r, cfg, grads->dy, "dy", e, cfg->C, false);
+    add_sequence(r, cfg, grads->dx, "dx", e, cfg->C, true);
+    add_sequence(r, cfg, grads->dg, "dg", e, cfg->C, true);
+    r.add("states", io->states, rows * recur_chunks(cfg->T), false);
+  }
+  r.add("dh_last", grads->dh_last, rows, false, kFirstAndLast);
+  r.add("dh0", grads->dh0, rows, true, kFirstAndLast);
+  r.add("dbias", grads->dbias, (int64_t)cfg->P * cfg->C * 4, true);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
   a.dy = grads->dy; a.dx = grads->dx; a.dg = grads->dg;
   a.dh_last = grads->dh_last; a.dh0 = grads->dh0; a.dbias = grads->dbias;
   a.ws = (float*)workspace;
@@ -238,6 +287,10 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
       (rc = check_floats(state, "state", true)) != POP_OK || (rc = check_floats(slots, "slots", false)) != POP_OK)
     return rc;
   if (n_slots < 1) return fail_thread(POP_EINVAL, "n_slots must be positive");
+  Regions r = recurrence_regions(cfg, io, true, kStep);
+  r.add("slots", slots, (int64_t)cfg->P * cfg->batch * 4, false);
+  r.add("state", state, (int64_t)cfg->P * n_slots * cfg->C * 4, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
   a.state = state; a.n_slots = n_slots; a.slots = slots;
   return launched(launch_recur_step(a, cfg->dtype, (hipStream_t)hip_stream));
 }
@@ -257,9 +310,13 @@ int pop_orthogonalize(const pop_ns_config* cfg, int32_t count, int32_t rows, int
   if ((rc = check_matrices(count, rows, cols, *g, "g", false, element_bytes(dtype))) != POP_OK ||
       (rc = check_matrices(count, rows, cols, *out, "out", true, element_bytes(dtype))) != POP_OK)
     return rc;
-  if (g->data == out->data && (g->matrix != out->matrix || g->row != out->row))
-    return fail_thread(POP_EINVAL, "out may be g only with the same strides");
-  if ((rc = check_workspace(workspace, workspace_bytes, ns_workspace_bytes(count, rows, cols))) != POP_OK) return rc;
+  const int64_t need = ns_workspace_bytes(count, rows, cols);
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  Regions r;
+  add_matrices(r, count, rows, cols, *g, "g", element_bytes(dtype), false, 1);
+  add_matrices(r, count, rows, cols, *out, "out", element_bytes(dtype), true, 1);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
   n.n_layers = 1;
   NsLayer& l = n.layer[0];
   l.rows = rows; l.cols = cols; l.count = count;
@@ -281,6 +338,8 @@ int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const p
   n.n_layers = n_layers;
   n.nesterov = nesterov != 0;
   n.hparams = (const float*)hparams;
+  Regions r;
+  r.add("hparams", hparams, (int64_t)P * sizeof(pop_muon_hparams), false);
   for (int k = 0; k < n_layers; ++k) {
     const pop_muon_layer& m = layers[k];
     if ((rc = check_matrices(P, m.rows, m.cols, m.grad, "grad", false, element_bytes(dtype))) != POP_OK ||
@@ -288,15 +347,18 @@ int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const p
         (rc = check_matrices(P, m.rows, m.cols, m.weight, "weight", true, 4)) != POP_OK)
       return rc;
     if (!isfinite(m.scale)) return fail_thread(POP_EINVAL, "layer %d: scale is not finite", k);
-    if (m.momentum.data == m.weight.data || m.grad.data == m.weight.data || m.grad.data == m.momentum.data)
-      return fail_thread(POP_EINVAL, "layer %d: grad, momentum and weight must not overlap", k);
     NsLayer& l = n.layer[k];
     l.rows = m.rows; l.cols = m.cols; l.count = P; l.scale = m.scale;
     l.g = m.grad.data; l.g_matrix = m.grad.matrix; l.g_row = m.grad.row;
     l.momentum = (float*)m.momentum.data; l.m_matrix = m.momentum.matrix; l.m_row = m.momentum.row;
     l.weight = (float*)m.weight.data; l.w_matrix = m.weight.matrix; l.w_row = m.weight.row;
+    add_matrices(r, P, m.rows, m.cols, m.grad, "a layer's grad", element_bytes(dtype), false);
+    add_matrices(r, P, m.rows, m.cols, m.momentum, "a layer's momentum", 4, true);
+    add_matrices(r, P, m.rows, m.cols, m.weight, "a layer's weight", 4, true);
   }
   if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
   return launched(launch_ns(n, dtype, workspace, (hipStream_t)hip_stream));
 }
 
