@@ -354,7 +354,9 @@ enum { POP_F32 = 0, POP_BF16 = 1, POP_F16 = 2 };   /* element types */
  *
  * with h_{-1} = h0 and, where reset_t is not zero, 0 in place of h_{t-1} (an episode starts at t).  Steps from a
  * sequence's length on are not used; y is 0 there and so are the gradients.  States, sums and gates are fp32
- * whatever the arrays' type; values are rounded once, when they are stored. */
+ * whatever the arrays' type; values are rounded once, when they are stored.
+ *
+ * POP_EUNSUPPORTED: T beyond 2^22; P * batch * C from 2^31 on, for whole sequences beyond 2^28. */
 typedef struct {
   int32_t P, batch;     /* agents, sequences of each agent */
   int32_t T;            /* steps (0 is legal: h_last = h0) */
@@ -394,7 +396,6 @@ typedef struct {
 int64_t pop_recurrence_workspace_bytes(const pop_recurrence_config* cfg);
 int64_t pop_recurrence_states_bytes(const pop_recurrence_config* cfg);
 
-/* POP_EUNSUPPORTED, as by the backward pass, for more than 2^28 sequences times channels. */
 int pop_recurrence_forward(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
                            void* workspace, int64_t workspace_bytes, void* hip_stream);
 
@@ -416,8 +417,11 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  *
  * which drives the singular values of G towards 1.  All sums are fp32 (|G|: fp64).  Products run on the fp16 matrix
  * instructions from operands split into two halves of 11 bits each, which is fp32's precision up to the last bits; calls
- * whose matrices all have at most 64 rows or columns run in fp64, unless the steps together multiply small singular values by
- * more than 2^20 (five steps of 3.4445, -4.775, 2.0315: 2^8.9). */
+ * whose matrices all have at most 64 rows or columns (the smaller side) run in fp64, unless the steps together multiply small singular values by
+ * more than 2^20 (five steps of 3.4445, -4.775, 2.0315: 2^8.9).
+ *
+ * POP_EUNSUPPORTED: rows or cols beyond 16384; matrices of one shape that together need 2^21 workgroups or more, which is
+ * about 2^33 elements in large matrices and 2^20 matrices in small ones. */
 enum { POP_NS_MAX_STEPS = 16 };
 typedef struct {
   int32_t steps;                        /* 0 .. POP_NS_MAX_STEPS */

@@ -23,7 +23,7 @@
 // are too many or too steep (below, k_gram64).  (Beside larger matrices small ones cost nothing, and launches of their own would.)
 //
 // Products on v_mfma_f32_32x32x16_f16 from operands in two fp16 halves, x = hi + lo with 11 bits each, held in units
-// (powers of two, Units below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
+// (powers of two, unit_of below) that keep the largest possible entry just below 2^15, so that lo keeps its bits for
 // entries down to 2^-14 of the largest: x y = hi hi + hi lo + lo hi, what is left out is below 2^-22 |x y|.  Three
 // instructions in place of sixteen of the fp32 ones.  The matrix pipe rounds its accumulator after every instruction: the
 // two small products have one of their own, so that a sum is rounded a third as often.
@@ -32,6 +32,7 @@
 // of 8 halves (lane l: row l & 31, indices 8 (l >> 5) ..), the hi block in front of the lo block, 2 KB together,
 // blocks of one row band adjacent.  Both operands have the contraction index inside, so X is kept in both orders.
 #include <hip/hip_runtime.h>
+#include <initializer_list>
 #include <type_traits>
 #include "operators.h"
 #include "pop_dev.h"
@@ -1254,6 +1255,17 @@ template <typename G> hipError_t run(const NsCall& c, char* ws, hipStream_t stre
 
 }  // namespace ns
 }  // namespace
+
+// k_norms; k_start; k_tile of 128 x 128, two of whose products may share a launch; k_square64 (of 512 work items) and k_last64.  The
+// other tilings are those of launches of few tiles (launch_product).
+int64_t ns_most_workgroups(int64_t rows, int64_t cols) {
+  const ns::Place p = ns::place_of((int)rows, (int)cols);
+  const int64_t mt = (p.mb + ns::kTile - 1) / ns::kTile, nt = (p.nb + ns::kTile - 1) / ns::kTile, n = rows < cols ? cols : rows;
+  int64_t most = ns::parts((int)rows, (int)cols);
+  for (const int64_t w : {(int64_t)p.mb * p.nb / 4 + 1, mt * (mt + 1), mt * nt, p.mb <= ns::kSmall ? (n + ns::kChunk - 1) / ns::kChunk : 0})
+    if (w > most) most = w;
+  return most;
+}
 
 int64_t ns_workspace_bytes(int count, int rows, int cols) {
   const ns::Place p = ns::place_of(rows, cols);

@@ -11,7 +11,8 @@ namespace op {
 constexpr int64_t kAlignment = 256;          // of a workspace
 // a launch's work items per grid dimension stay below 2^32: one per column in a single step, up to eight over sequences
 constexpr int64_t kMaxLanes = 1ll << 31, kMaxColumns = 1ll << 28;
-constexpr int kMaxSteps = 1 << 22;           // chunks of a sequence are a grid dimension of at most 65,535
+constexpr int kMaxSteps = 1 << 22;           // steps and tiles are counted in ints, with room to spare; longer sequences go in pieces
+constexpr int64_t kMaxWorkgroups = 1 << 21;  // of one layer's matrices
 
 constexpr double kMostSingular = 8.0;
 
@@ -139,8 +140,10 @@ int check_ns(const pop_ns_config* c, int32_t dtype, bool three, NsCall& n) {
 int check_shape(int64_t count, int64_t rows, int64_t cols) {
   if (count < 1 || rows < 1 || cols < 1) return fail_thread(POP_EINVAL, "a matrix count, rows or cols is not positive");
   if (rows > kNsMaxSide || cols > kNsMaxSide) return fail_thread(POP_EUNSUPPORTED, "rows and cols must be at most %d", kNsMaxSide);
-  // a launch has at most two workgroups per 32 x 32 block of each of 8 layers; its work items stay below 2^32
-  if ((count + 7) * ((rows + 31) / 32) * ((cols + 31) / 32) >= 1 << 20) return fail_thread(POP_EUNSUPPORTED, "more than 2^20 blocks of 32 x 32 in %lld matrices", (long long)count);
+  // a launch's work items, 256 for each workgroup of up to 8 layers, stay below 2^32
+  const int64_t most = ns_most_workgroups(rows, cols);
+  if (count >= kMaxWorkgroups / most || (count * most + 7) / 8 * 8 >= kMaxWorkgroups)
+    return fail_thread(POP_EUNSUPPORTED, "%lld matrices of %lld x %lld need 2^21 workgroups or more", (long long)count, (long long)rows, (long long)cols);
   return POP_OK;
 }
 

@@ -64,6 +64,7 @@ struct NsCall {
   float q_most[POP_NS_MAX_STEPS];    // within which the steps of a segment up to step k multiply a singular value
   NsLayer layer[POP_MUON_MAX_LAYERS];
 };
+int64_t ns_most_workgroups(int64_t rows, int64_t cols);         // of one matrix, in units of 256 work items, in any launch
 int64_t ns_workspace_bytes(int count, int rows, int cols);      // of one layer, a multiple of 256
 hipError_t launch_ns(const NsCall& c, int dtype, void* ws, hipStream_t s);
 
