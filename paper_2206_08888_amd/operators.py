@@ -29,6 +29,13 @@ def _dtype_code(dtype):
     return DTYPE_CODES[dtype]
 
 
+def _sizes(*sizes):
+    """The boundary's numbers are of 32 bits, and ctypes cuts off what does not fit."""
+    for v in sizes:
+        if not -1 << 31 <= v < 1 << 31:
+            raise ValueError("size %d does not fit in 32 bits" % v)
+
+
 # current_stream(index).cuda_stream, where PyTorch has it without the object around it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -94,6 +101,7 @@ class Recurrence(_Operator):
 
     def __init__(self, P, batch, T, C, dtype=torch.float32, device="cuda"):
         super().__init__(dtype, device)
+        _sizes(P, batch, T, C)
         self.P, self.batch, self.T, self.C = P, batch, T, C
         self._rows, self._channels = (P, batch, C), (P, C)
         self._cfg = pop_recurrence_config(P, batch, T, C, self.code, 0)
@@ -163,6 +171,8 @@ class Recurrence(_Operator):
         if not isinstance(state, torch.Tensor) or state.dim() != 3:
             raise ValueError("state must be a [P, n_slots, C] tensor")
         n_slots = state.shape[1]
+        if n_slots >> 31:
+            _sizes(n_slots)
         if slots is None and n_slots < self.batch:
             raise ValueError("state has %d rows for %d sequences and no slots are given" % (n_slots, self.batch))
         xs, gs = self._sequence(x, "x", shape), self._sequence(g, "g", shape)
@@ -190,6 +200,7 @@ class Orthogonalizer(_NewtonSchulz):
 
     def __init__(self, count, rows, cols, dtype=torch.float32, device="cuda", steps=5, coef=NS_COEF, eps=1e-7):
         super().__init__(dtype, device)
+        _sizes(count, rows, cols)
         self.shape = (count, rows, cols)
         self._ns = make_ns_config(steps, coef, eps)
         self._bytes = _check(self.lib.pop_orthogonalize_workspace_bytes(count, rows, cols))
@@ -220,6 +231,7 @@ class Muon(_NewtonSchulz):
     def __init__(self, P, shapes, dtype=torch.float32, device="cuda", scales=None, nesterov=True, steps=5, coef=NS_COEF, eps=1e-7):
         super().__init__(dtype, device)
         self.P, self.shapes, self.nesterov = P, [tuple(s) for s in shapes], nesterov
+        _sizes(P, *(n for s in self.shapes for n in s))
         scales = [max(1.0, c / r) ** 0.5 for r, c in self.shapes] if scales is None else list(scales)
         if len(scales) != len(self.shapes):
             raise ValueError("%d scales for %d layers" % (len(scales), len(self.shapes)))
