@@ -82,6 +82,8 @@ class Agents:
 
 def train(P=8, width=64, T=40, batch=32, updates=150, lr=None, device="cuda", seed=0):
     """(losses of the first and of the last update, share of cues recalled per agent, agents)."""
+    if updates < 1:
+        raise ValueError("updates must be positive, not %d" % updates)
     lr = torch.logspace(-1.5, -0.9, P) if lr is None else lr
     agents, gen = Agents(P, width, T, batch, lr, device, seed), torch.Generator(device=device)
     gen.manual_seed(seed + 1)

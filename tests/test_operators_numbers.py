@@ -28,3 +28,10 @@ def test_states(lib):  # noqa: F811
     state = torch.empty((2, FAR + 3, 4), device="meta")
     with pytest.raises(ValueError, match="32 bits"):
         plan.step(torch.empty((2, 3, 4), device="meta"), torch.empty((2, 3, 4), device="meta"), state)
+
+
+@pytest.mark.parametrize("updates", [0, -1])
+def test_an_example_without_updates(lib, updates):  # noqa: F811
+    from paper_2206_08888_amd import recall
+    with pytest.raises(ValueError, match="updates"):
+        recall.train(updates=updates)
