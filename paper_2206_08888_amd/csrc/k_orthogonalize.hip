@@ -1155,9 +1155,12 @@ Args args_of(int step, int first, int last, int xt) {
 // / 9.7, 80: 14.8 / 14.5 / 15.8, 160: 24.3 / 27.0 / 28.5; X = Q X of 20: 13.3 / 10.2 / 12.4, 40: 14.2 / 14.6 / 16.2, 80: 23.0 /
 // 21.5 / 27.6; four of 1024 x 4096: X X^T 108 / 113 / 120, X = Q X 127 / 150 / 223; one of 2048 x 2048: 54 / 58 / 73.
 // Triangles, whose light halves come last, keep halves up to 400 tiles (all steps of fp32 calls, 128 x 128 / halves): 272 tiles
-// (two of 2048 x 2048) 1443 / 1304, 288 (eight of 1024 x 1024) 793 / 736, 300 (100 of 256 x 256) 331 / 303, 390 404 / 400, 408
-// (three of 2048 x 2048) 1793 / 1873, 500 (50 of 512 x 512) 771 / 787.
-constexpr int kTilesFrom = 256, kTrianglesFrom = 400, kHalvesFrom = 128, kQuadsFrom = 128;
+// (two of 2048 x 2048) 1445 / 1314, 288 (eight of 1024 x 1024) 794 / 732, 300 (100 of 256 x 256) 335 / 304, 390 (130) 402 / 398; of
+// 400, 40 of 512 x 512 661 / 663, 40 of 400 x 640 588 / 578, 80 policies of 17 x 256, 256 x 256 and 256 x 6 332 / 315.  Beyond, either is
+// ahead by up to 5 %, as the last workgroups fill the CUs: 408 (three of 2048 x 2048) 1792 / 1876, 432 (twelve of 1024 x 1024) 1014 /
+// 1044, 500 (50 of 512 x 512) 774 / 792, 600 (60) 925 / 884, 800 (80) 1186 / 1205, 500 (100 policies) 404 / 376; from 1000 on whole
+// tiles: 1008 (28 of 1024 x 1024) 2397 / 2510, 1200 (400 of 256 x 256) 1177 / 1216, 1280 (256 policies) 936 / 975.
+constexpr int kTilesFrom = 256, kTrianglesFrom = 401, kHalvesFrom = 128, kQuadsFrom = 128;
 
 template <int MODE, typename G, typename E, typename N>
 void launch_product(const NsCall& c, Args a, const E& ends, char* ws, hipStream_t stream, N count) {
