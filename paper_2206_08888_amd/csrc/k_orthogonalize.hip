@@ -8,15 +8,15 @@
 //
 //   A = X X^T;  per step of a segment:  Q = P Q,  A = P A P;  then X = Q X
 //
-// so that X, m x n, is touched twice per segment.  An error of A grows by up to k0^2 per step inside one.  Errors against
-// 64 bits, segments of 1 / 2 / 3 steps, over those of fp32 products: 0.78 / 1.6 / 2.6 in the mean of 40 shapes, 3 / 8 / 66 at
-// most (small square matrices, one of whose singular values is small).  So results in fp32 take one step per segment,
-// and results of 16 bits, whose rounding is 2e-4 or more, three where that is less work, from n = 1.5 m on (four 1024 x
-// 4096: 877 us, with one step 1286; 256 x 256: 114, with one 102).  Steep steps enlarge the difference: errors of A, 2^-22 of
-// its largest entries, are multiplied by what a step multiplies A by, the square of its slope at 0 and about.  Segments of
-// three are taken while all steps together multiply A by at most 2^22 (kSegmentGain squared; five and six steps of the usual
-// quintic: 2^17.8 and 2^21.4); eight of slope 5, 2^37, had up to 16 times the error of fp32 products, with one step less than
-// theirs.
+// so that X, m x n, is touched twice per segment.  Errors against 64 bits, segments of 1 / 2 / 3 steps, over those of fp32
+// products: 0.42 / 0.83 / 1.13 in the mean of 60 shapes from m = 65 on (ordinary gradients, the usual quintic, five steps), 0.71 /
+// 4.2 / 3.0 at most, the larger ones on square matrices; of n >= 1.5 m 0.71 / 1.9 / 1.7 at most.  So results in fp32 take one step
+// per segment, and results of 16 bits, whose rounding is 2e-4 or more, three where that is less work, from n = 1.5 m on
+// (four 1024 x 4096: 840 us, with one step 1270; 256 x 256: 114, with one 102).  Steep steps enlarge the difference: a step
+// multiplies errors of A, 2^-22 of its largest entries, by the square of its slope at 0, what is unsymmetric in them (blocks
+// on the diagonal are not mirrored inside) by the third power.  Segments of three are taken while all steps together
+// multiply A by at most 2^22 (kSegmentGain squared; five and six steps of the usual quintic: 2^17.8 and 2^21.4); eight of slope 5,
+// 2^37, had up to 16 times the error of fp32 products, with one step less than theirs.
 //
 // All matrices of a call advance together, a launch per product.  Calls whose matrices all have m up to 64 take a path of
 // their own: the squares of A, Q and so on fit a workgroup, and with everything in 64 bits all steps are one segment, unless they
@@ -1080,7 +1080,7 @@ __global__ void __launch_bounds__(kThreads) k_last64(Args c, Ends ends, char* ws
   } else {
     for (int k = 0; k < m; ++k) {
       const double a = x[k][lane];
-      const double* b = q + k * w.side + first;             // up to 15 doubles behind the square's last row: q has 64 x 64
+      const double* b = q + k * w.side + first;             // first < m, and the side is a multiple of 16
 #pragma unroll
       for (int r = 0; r < 16; ++r) v[r] = fma(a, b[r], v[r]);
     }

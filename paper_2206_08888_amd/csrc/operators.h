@@ -16,7 +16,7 @@ constexpr int kRecurChunk = 128;     // steps between the states that forward le
 
 struct RecurArgs {
   int P, B, T, C;
-  pop_sequence x, g, y, reset;       // step strides of single-step calls are set by the boundary
+  pop_sequence x, g, y, reset;       // single steps use no step strides
   const float *bias, *h0;
   const int32_t* lengths;
   float *h_last, *states;            // states: [P * B, chunks, C], the state before each chunk
