@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(kThreads) k_quad(Args c, E ends, char* ws) {
 // 2048 matrices 128 x 128 tiles run at 840 TFLOP/s of fp16 products, prologue and epilogue included, where a large fp16
 // product of the library reaches 1130.  Four of 1024 x 4096: X = Q X 127 us, 815 TFLOP/s; X X^T 100, 580, and
 // squares of A 31, 470, as 288 half tiles on 256 CUs leave some with two.  Products of 256 x 256 (80 of them:
-// X X^T 20, B 18, X 25) are short of stages, eight, beside their prologue and epilogue.  Eight wavefronts with both operands
+// as halves X X^T 16, B 16, whole X 25) are short of stages, eight, beside their prologue and epilogue.  Eight wavefronts with both operands
 // in LDS: the same time; four wavefronts so: 395 against 358 us a step of 80 agents.
 //
 // Halves of tiles on the diagonal: the left one's lower blocks are the right one's upper blocks mirrored and are not
@@ -842,9 +842,10 @@ __global__ void __launch_bounds__(kTileThreads, 2) k_tile(Args c, E ends, char* 
 
 // The 64-bit path: k_gram64 updates the momentum and sums U U^T over a piece of n, k_square64 adds the pieces up (the trace
 // is |U|^2), takes all steps as Q of U U^T / (|U| + eps)^2, and k_last64 multiplies Q by U.  Three launches, in which k_square64's
-// products, one after the other in one workgroup per matrix, are the longest part: 8 of 17 x 2000 30 us (48 as fp16 halves
-// in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 77 (58).  That part on vector instructions made it 119, on the
-// matrix ones with a wavefront's tiles one by one 159, its chains interleaved 92, from eight wavefronts 77.
+// products, one after the other in one workgroup per matrix, are the longest part: 8 of 17 x 2000 31 us (48 as fp16 halves
+// in segments of three), 6 of 3 x 740 21 (44), 8 of 64 x 2048 80 (58).  That part on vector instructions made it 119, on the
+// matrix ones with a wavefront's tiles one by one 159, its chains interleaved 92, from eight wavefronts 77, with tiles on
+// the diagonal mirrored 80.
 //
 // What rounding makes of an eigenvalue of zero, about 2^-53 of either sign, grows with every step as small eigenvalues do.
 // Large, it is an error of its size; far below zero, steps diverge.  So the path is taken while all steps together multiply
