@@ -140,9 +140,8 @@ int check_ns(const pop_ns_config* c, int32_t dtype, bool three, NsCall& n) {
 int check_shape(int64_t count, int64_t rows, int64_t cols) {
   if (count < 1 || rows < 1 || cols < 1) return fail_thread(POP_EINVAL, "a matrix count, rows or cols is not positive");
   if (rows > kNsMaxSide || cols > kNsMaxSide) return fail_thread(POP_EUNSUPPORTED, "rows and cols must be at most %d", kNsMaxSide);
-  // a launch's work items, 256 for each workgroup of up to 8 layers, stay below 2^32
-  const int64_t most = ns_most_workgroups(rows, cols);
-  if (count >= kMaxWorkgroups / most || (count * most + 7) / 8 * 8 >= kMaxWorkgroups)
+  // a launch's work items, 256 for each workgroup of up to 8 layers, stay below 2^32 (a layer's workgroups are a multiple of 8)
+  if ((count + 7) / 8 * 8 * ns_most_workgroups(rows, cols) >= kMaxWorkgroups)
     return fail_thread(POP_EUNSUPPORTED, "%lld matrices of %lld x %lld need 2^21 workgroups or more", (long long)count, (long long)rows, (long long)cols);
   return POP_OK;
 }
