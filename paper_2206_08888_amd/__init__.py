@@ -4,7 +4,8 @@ The computation lives entirely in libpop.so (hand-written gfx950 kernels);
 this package only marshals arguments.  PyTorch is used by callers to allocate
 the device workspace and to supply a stream.
 """
-from importlib import import_module
+from importlib import import_module as _import_module
+from importlib.util import find_spec as _find_spec
 
 from .binding import (  # noqa: F401
     POP_ALGO_SAC, POP_ALGO_TD3, POP_ALGO_TD3_SHARED, POP_LAUNCH_AUTO, POP_LAUNCH_PER_PART, POP_LAUNCH_SINGLE, POP_LAUNCH_TAIL,
@@ -18,13 +19,14 @@ from .binding import (  # noqa: F401
 )
 
 _ON_TENSORS = ("Muon", "Orthogonalizer", "Recurrence", "operators")
+__all__ = [name for name in globals() if not name.startswith("_")] + list(_ON_TENSORS if _find_spec("torch") else ())
 
 
 def __getattr__(name):
     """The operators on tensors, which need PyTorch, when they are first asked for: the rest does without it."""
     if name not in _ON_TENSORS:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
-    module = import_module(".operators", __name__)
+    module = _import_module(".operators", __name__)
     return module if name == "operators" else getattr(module, name)
 
 

@@ -27,6 +27,14 @@ def test_operators_on_tensors_say_what_is_missing():
     assert r.returncode != 0 and "ModuleNotFoundError" in r.stderr and "torch" in r.stderr
 
 
+def test_all_names_at_once():
+    names = {}
+    exec("from paper_2206_08888_amd import *", names)
+    assert names["Muon"] is pp.Muon and names["pop_update"] is pp.pop_update and "import_module" not in names
+    r = _run("from paper_2206_08888_amd import *\nprint(POP_F32, make_config)")
+    assert r.returncode == 0, r.stderr
+
+
 def test_every_name_is_found():
     for name in ("Recurrence", "Orthogonalizer", "Muon", "NS_COEF", "make_ns_config", "pop_sequence", "pop_muon_layer", "POP_F16", "operators"):
         assert getattr(pp, name) is not None and name in dir(pp)
