@@ -411,6 +411,67 @@ int pop_recurrence_backward(const pop_recurrence_config* cfg, const pop_recurren
 int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_io* io,
                         float* state, int32_t n_slots, const int32_t* slots, void* hip_stream);
 
+/* Linear attention with a decay for each head: a matrix S [key_dim, value_dim] for a memory, per agent i, sequence b, head h:
+ *
+ *   S_t = lambda * S_{t-1} + k_t v_t^T,   o_t = scale * S_t^T q_t     for 0 <= t < length,   lambda = exp(log_decay[i, h])
+ *
+ * with S_{-1} = state0 and, where reset_t is not zero, 0 in place of S_{t-1}.  Steps from a sequence's length on are not used;
+ * o is 0 there and so are the gradients.  States and sums are fp32 whatever the arrays' type.  An infinity or a NaN reaches the steps
+ * that the formula lets it reach and no others: not earlier ones, and none behind a reset.
+ *
+ * POP_EUNSUPPORTED: key_dim or value_dim beyond 128, T beyond 2^22, P * batch * heads from 2^24 on. */
+enum { POP_LINEAR_MAX_DIM = 128 };
+typedef struct {
+  int32_t P, batch;              /* agents, sequences of each agent */
+  int32_t T;                     /* steps (0 is legal: state_last = state0) */
+  int32_t heads;
+  int32_t key_dim, value_dim;    /* channels of q and k, of v and o */
+  int32_t dtype;                 /* POP_F32, POP_BF16 or POP_F16: q, k, v, o and their gradients */
+  float scale;
+} pop_linear_config;
+
+/* A [P, batch, T, heads, channels] array: channels adjacent, the other axes with strides in elements (zero: the axis is
+ * broadcast, for inputs only; outputs must not overlap themselves, each other, any input or the workspace: POP_EINVAL). */
+typedef struct {
+  void* data;
+  int64_t agent, row, step, head;
+} pop_heads;
+
+typedef struct {
+  pop_heads q, k, v;
+  pop_heads o;               /* written (pop_linear_backward ignores it) */
+  pop_sequence reset;        /* uint8 [P, batch, T], or data NULL: no resets */
+  const float* log_decay;    /* [P, heads], taken as if within -200 .. 0, or NULL: zeros (nothing decays) */
+  const float* state0;       /* [P, batch, heads, key_dim, value_dim], or NULL: zeros */
+  float* state_last;         /* written by forward: the state behind the last step, or NULL; may be state0 */
+  const int32_t* lengths;    /* [P, batch], taken as if within 0 .. T, or NULL: T */
+} pop_linear_io;
+
+typedef struct {
+  pop_heads d_o;             /* gradient of o */
+  pop_heads dq, dk, dv;      /* written; of an input with broadcast axes, too, for each of its uses */
+  const float* dstate_last;  /* gradient of state_last, or NULL: zeros */
+  float* dstate0;            /* written: gradient of state0, or NULL */
+} pop_linear_grads;
+
+/* Bytes of workspace of the two calls; negative POP_E* code on a bad config. */
+int64_t pop_linear_forward_workspace_bytes(const pop_linear_config* cfg);
+int64_t pop_linear_backward_workspace_bytes(const pop_linear_config* cfg);
+
+int pop_linear_forward(const pop_linear_config* cfg, const pop_linear_io* io,
+                       void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Gradients of sum(o * d_o) + sum(state_last * dstate_last), with q, k, v, reset, log_decay, state0 and lengths as forward had
+ * them; nothing else is kept from it (states are found again).  Decays are hyperparameters: they have no gradient. */
+int pop_linear_backward(const pop_linear_config* cfg, const pop_linear_io* io, const pop_linear_grads* grads,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* One step for acting agents: q, k, v, o are [P, batch, heads, channels] (cfg->T is 1, the step strides are ignored, reset is
+ * [P, batch]), the states live in state[P, n_slots, heads, key_dim, value_dim] and are updated in place.  slots as in
+ * pop_recurrence_step.  io->state0, state_last and lengths must be NULL. */
+int pop_linear_step(const pop_linear_config* cfg, const pop_linear_io* io,
+                    float* state, int32_t n_slots, const int32_t* slots, void* hip_stream);
+
 /* Orthogonalised updates.  For a matrix G of r x c, with |G| its Frobenius norm:
  *
  *   X = G / (|G| + eps);   `steps` times:  A = X X^T,  X = k0 X + (k1 A + k2 A A) X         (Newton-Schulz products)
@@ -468,6 +529,31 @@ int64_t pop_muon_workspace_bytes(int32_t P, int32_t n_layers, const pop_muon_lay
 int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const pop_muon_layer* layers, int32_t dtype,
                   int32_t nesterov, const pop_muon_hparams* hparams, void* workspace, int64_t workspace_bytes,
                   void* hip_stream);
+
+/* Norms of gradients, and clipping.  Over all of an agent's elements in all tensors of the call:
+ *
+ *   norm_i = sqrt(sum g^2),   out = f_i g,   f_i = 1 where norm_i + eps <= max_norm_i, else max_norm_i / (norm_i + eps)
+ *
+ * Squares are summed in fp64, in an order that sizes alone decide; f_i is fp32, the product is rounded once.  A norm that is infinite or
+ * NaN is reported as it is, and the formula passes it on to the agent's gradients; other agents' are not touched by it.
+ * POP_EUNSUPPORTED: rows * cols beyond 2^40 for an agent's part of a tensor, 2^24 or more pieces of 2^13 elements in a call. */
+enum { POP_CLIP_MAX_TENSORS = 256 };
+
+/* One tensor of all agents' gradients [P, rows, cols]; columns adjacent, strides in elements. */
+typedef struct {
+  int32_t rows, cols;
+  int32_t dtype;             /* tensors of one call may differ in type */
+  int32_t reserved_;
+  pop_matrices grad;         /* read */
+  pop_matrices out;          /* written unless max_norm is NULL, of the same type: may be grad (with the same strides) */
+} pop_gradient;
+
+/* Bytes of workspace for tensors of these shapes (only rows, cols and dtype are read). */
+int64_t pop_clip_workspace_bytes(int32_t P, int32_t n_tensors, const pop_gradient* grads);
+
+/* max_norm: [P] floats in device memory, not negative, or NULL: norms only.  norms: [P], written, or NULL.  eps: not negative, finite. */
+int pop_clip_gradients(int32_t P, int32_t n_tensors, const pop_gradient* grads, double eps, const float* max_norm, float* norms,
+                       void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /* Message of the last failing call on this context (of the last failing pop_create, pop_workspace_bytes,
  * pop_net_size or operator of this thread when ctx is NULL).  Valid until the next call on the context. */

@@ -16,9 +16,10 @@ from .binding import (  # noqa: F401
     pop_workspace_bytes, pop_config, pop_hparams, pop_tuning,
     NS_COEF, POP_BF16, POP_F16, POP_F32, make_ns_config, pop_matrices, pop_muon_layer, pop_ns_config, pop_recurrence_config,
     pop_recurrence_grads, pop_recurrence_io, pop_sequence,
+    pop_gradient, pop_heads, pop_linear_config, pop_linear_grads, pop_linear_io,
 )
 
-_ON_TENSORS = ("Muon", "Orthogonalizer", "Recurrence", "operators")
+_ON_TENSORS = ("GradientClip", "LinearAttention", "Muon", "Orthogonalizer", "Recurrence", "operators")
 __all__ = [name for name in globals() if not name.startswith("_")] + list(_ON_TENSORS if _find_spec("torch") else ())
 
 

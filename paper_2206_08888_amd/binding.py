@@ -73,7 +73,26 @@ class pop_recurrence_grads(C.Structure):
                 ("dh0", C.c_void_p), ("dbias", C.c_void_p)]
 
 
-NS_MAX_STEPS, MUON_MAX_LAYERS = 16, 8
+class pop_linear_config(C.Structure):
+    _fields_ = [("P", C.c_int32), ("batch", C.c_int32), ("T", C.c_int32), ("heads", C.c_int32), ("key_dim", C.c_int32),
+                ("value_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class pop_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("agent", C.c_int64), ("row", C.c_int64), ("step", C.c_int64), ("head", C.c_int64)]
+
+
+class pop_linear_io(C.Structure):
+    _fields_ = [("q", pop_heads), ("k", pop_heads), ("v", pop_heads), ("o", pop_heads), ("reset", pop_sequence),
+                ("log_decay", C.c_void_p), ("state0", C.c_void_p), ("state_last", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class pop_linear_grads(C.Structure):
+    _fields_ = [("d_o", pop_heads), ("dq", pop_heads), ("dk", pop_heads), ("dv", pop_heads), ("dstate_last", C.c_void_p),
+                ("dstate0", C.c_void_p)]
+
+
+NS_MAX_STEPS, MUON_MAX_LAYERS, CLIP_MAX_TENSORS = 16, 8, 256
 NS_COEF = (3.4445, -4.7750, 2.0315)                      # five steps take singular values of 0.01 .. 1 to 0.7 .. 1.2
 
 
@@ -88,6 +107,11 @@ class pop_matrices(C.Structure):
 class pop_muon_layer(C.Structure):
     _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("scale", C.c_float), ("reserved_", C.c_int32),
                 ("grad", pop_matrices), ("momentum", pop_matrices), ("weight", pop_matrices)]
+
+
+class pop_gradient(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("dtype", C.c_int32), ("reserved_", C.c_int32),
+                ("grad", pop_matrices), ("out", pop_matrices)]
 
 
 def make_ns_config(steps=5, coef=NS_COEF, eps=1e-7):
@@ -165,6 +189,13 @@ def load_library(path=None):
         "pop_recurrence_forward": (C.c_int, [vp, vp, vp, i64, vp]),
         "pop_recurrence_backward": (C.c_int, [vp, vp, vp, vp, i64, vp]),
         "pop_recurrence_step": (C.c_int, [vp, vp, vp, i32, vp, vp]),
+        "pop_linear_forward_workspace_bytes": (i64, [vp]),
+        "pop_linear_backward_workspace_bytes": (i64, [vp]),
+        "pop_linear_forward": (C.c_int, [vp, vp, vp, i64, vp]),
+        "pop_linear_backward": (C.c_int, [vp, vp, vp, vp, i64, vp]),
+        "pop_linear_step": (C.c_int, [vp, vp, vp, i32, vp, vp]),
+        "pop_clip_workspace_bytes": (i64, [i32, i32, vp]),
+        "pop_clip_gradients": (C.c_int, [i32, i32, vp, C.c_double, vp, vp, vp, i64, vp]),
         "pop_orthogonalize_workspace_bytes": (i64, [i32, i32, i32]),
         "pop_orthogonalize": (C.c_int, [vp, i32, i32, i32, i32, vp, vp, vp, i64, vp]),
         "pop_muon_workspace_bytes": (i64, [i32, i32, vp]),

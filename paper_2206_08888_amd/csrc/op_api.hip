@@ -14,6 +14,9 @@ constexpr int64_t kMaxLanes = 1ll << 31, kMaxColumns = 1ll << 28;
 constexpr int kMaxSteps = 1 << 22;           // steps and tiles are counted in ints, with room to spare; longer sequences go in pieces
 constexpr int64_t kMaxWorkgroups = 1 << 21;  // of one layer's matrices
 
+constexpr int64_t kMaxLinearRows = 1 << 24;  // P * batch * heads: 256 work items each
+constexpr int64_t kMaxElements = 1ll << 40, kMaxPieces = 1 << 24;
+
 constexpr double kMostSingular = 8.0;
 
 int64_t element_bytes(int32_t dtype) { return dtype == POP_F32 ? 4 : 2; }
@@ -41,7 +44,7 @@ int check_floats(const void* p, const char* name, bool needed) {
 // Whether an array of n[i] blocks at stride[i] with `inner` adjacent elements surely has no element twice.
 bool apart(int64_t inner, int axes, const int64_t* n, const int64_t* stride) {
   int64_t extent = inner;
-  bool done[3] = {false, false, false};
+  bool done[kAxes] = {};
   for (int k = 0; k < axes; ++k) {
     int next = -1;
     int64_t least = 0;
@@ -73,7 +76,7 @@ int check_workspace(void* p, int64_t have, int64_t need) {
   return POP_OK;
 }
 
-int check_apart(const Regions& r) {
+template <typename R> int check_apart(R& r) {
   const char *one, *other;
   return r.clash(one, other) ? fail_thread(POP_EINVAL, "%s and %s overlap", one, other) : POP_OK;
 }
@@ -83,7 +86,7 @@ void add_sequence(Regions& r, const pop_recurrence_config* c, const pop_sequence
   r.add(name, s.data, inner * bytes, 3, n, stride, written, same);
 }
 
-void add_matrices(Regions& r, int64_t count, int64_t rows, int64_t cols, const pop_matrices& m, const char* name, int64_t bytes, bool written, int same = 0) {
+template <typename R> void add_matrices(R& r, int64_t count, int64_t rows, int64_t cols, const pop_matrices& m, const char* name, int64_t bytes, bool written, int same = 0) {
   const int64_t n[2] = {count, rows}, stride[2] = {m.matrix * bytes, m.row * bytes};
   r.add(name, m.data, cols * bytes, 2, n, stride, written, same);
 }
@@ -204,6 +207,99 @@ Regions recurrence_regions(const pop_recurrence_config* c, const pop_recurrence_
 }
 enum { kStep = 1, kFirstAndLast = 2 };       // Region::same
 
+// ---- linear attention
+
+int check_linear(const pop_linear_config* c) {
+  if (!c) return fail_thread(POP_EINVAL, "config is NULL");
+  if (c->P < 1 || c->batch < 1 || c->heads < 1 || c->key_dim < 1 || c->value_dim < 1 || c->T < 0)
+    return fail_thread(POP_EINVAL, "config: P, batch, heads, key_dim and value_dim must be positive, T not negative");
+  if (c->dtype != POP_F32 && c->dtype != POP_BF16 && c->dtype != POP_F16) return fail_thread(POP_EINVAL, "config: unknown dtype %d", c->dtype);
+  if (!isfinite(c->scale)) return fail_thread(POP_EINVAL, "config: scale is not finite");
+  if (c->key_dim > POP_LINEAR_MAX_DIM || c->value_dim > POP_LINEAR_MAX_DIM)
+    return fail_thread(POP_EUNSUPPORTED, "key_dim and value_dim must be at most %d", (int)POP_LINEAR_MAX_DIM);
+  if (c->T > kMaxSteps) return fail_thread(POP_EUNSUPPORTED, "T must be at most %d", kMaxSteps);
+  if ((int64_t)c->P * c->batch >= kMaxLinearRows || (int64_t)c->P * c->batch * c->heads >= kMaxLinearRows)
+    return fail_thread(POP_EUNSUPPORTED, "P * batch * heads must be below 2^24");
+  return POP_OK;
+}
+
+int check_heads(const pop_linear_config* c, const pop_heads& s, int64_t channels, const char* name, bool output, int64_t bytes) {
+  if (!s.data) return fail_thread(POP_EINVAL, "%s is NULL", name);
+  if ((uintptr_t)s.data % bytes) return fail_thread(POP_EINVAL, "%s is not aligned to its type", name);
+  const int64_t n[4] = {c->P, c->batch, c->T, c->heads}, stride[4] = {s.agent, s.row, s.step, s.head};
+  if (output && !apart(channels, 4, n, stride)) return fail_thread(POP_EINVAL, "%s: its strides let elements overlap", name);
+  return POP_OK;
+}
+
+void add_heads(Regions& r, const pop_linear_config* c, const pop_heads& s, int64_t channels, const char* name, int64_t bytes, bool written) {
+  const int64_t n[4] = {c->P, c->batch, c->T, c->heads}, stride[4] = {s.agent * bytes, s.row * bytes, s.step * bytes, s.head * bytes};
+  r.add(name, s.data, channels * bytes, 4, n, stride, written);
+}
+
+int64_t linear_rows(const pop_linear_config* c) { return (int64_t)c->P * c->batch * c->heads; }
+int64_t linear_state_bytes(const pop_linear_config* c) { return (int64_t)c->key_dim * c->value_dim * 4; }
+
+// What forward, backward and single steps have in common, checked: config, inputs, decays, lengths; o where this call has it.
+int linear_common(const pop_linear_config* c, const pop_linear_io* io, bool o) {
+  int rc = check_linear(c);
+  if (rc != POP_OK) return rc;
+  if (!io) return fail_thread(POP_EINVAL, "io is NULL");
+  if ((rc = check_floats(io->log_decay, "log_decay", false)) != POP_OK || (rc = check_floats(io->state0, "state0", false)) != POP_OK ||
+      (rc = check_floats(io->state_last, "state_last", false)) != POP_OK || (rc = check_floats(io->lengths, "lengths", false)) != POP_OK)
+    return rc;
+  if (c->T == 0) return POP_OK;
+  const int64_t e = element_bytes(c->dtype);
+  if ((rc = check_heads(c, io->q, c->key_dim, "q", false, e)) != POP_OK || (rc = check_heads(c, io->k, c->key_dim, "k", false, e)) != POP_OK ||
+      (rc = check_heads(c, io->v, c->value_dim, "v", false, e)) != POP_OK || (o && (rc = check_heads(c, io->o, c->value_dim, "o", true, e)) != POP_OK))
+    return rc;
+  return POP_OK;
+}
+
+Regions linear_regions(const pop_linear_config* c, const pop_linear_io* io, bool o) {
+  Regions r;
+  const int64_t e = element_bytes(c->dtype), rows = (int64_t)c->P * c->batch;
+  if (c->T > 0) {
+    add_heads(r, c, io->q, c->key_dim, "q", e, false);
+    add_heads(r, c, io->k, c->key_dim, "k", e, false);
+    add_heads(r, c, io->v, c->value_dim, "v", e, false);
+    if (o) add_heads(r, c, io->o, c->value_dim, "o", e, true);
+    const int64_t n[3] = {c->P, c->batch, c->T}, stride[3] = {io->reset.agent, io->reset.row, io->reset.step};
+    r.add("reset", io->reset.data, 1, 3, n, stride, false);
+  }
+  r.add("log_decay", io->log_decay, (int64_t)c->P * c->heads * 4, false);
+  r.add("lengths", io->lengths, rows * 4, false);
+  return r;
+}
+
+LinearArgs linear_args(const pop_linear_config* c, const pop_linear_io* io) {
+  LinearArgs a = {};
+  a.P = c->P; a.B = c->batch; a.T = c->T; a.H = c->heads;
+  a.log_decay = io->log_decay; a.reset = io->reset; a.lengths = io->lengths;
+  return a;
+}
+
+int64_t linear_workspace(const pop_linear_config* c, bool backward) {
+  const int rc = check_linear(c);
+  return rc != POP_OK ? rc : linear_workspace_bytes(c->P, c->batch, c->T, c->heads, c->key_dim, c->value_dim, element_bytes(c->dtype), backward);
+}
+
+// ---- clipping
+
+int check_gradients(int32_t P, int32_t n, const pop_gradient* g) {
+  if (P < 1) return fail_thread(POP_EINVAL, "P must be positive");
+  if (n < 1 || n > POP_CLIP_MAX_TENSORS) return fail_thread(POP_EINVAL, "n_tensors must be 1 .. %d", (int)POP_CLIP_MAX_TENSORS);
+  if (!g) return fail_thread(POP_EINVAL, "grads is NULL");
+  int64_t pieces = 0;
+  for (int k = 0; k < n; ++k) {
+    if (g[k].rows < 1 || g[k].cols < 1) return fail_thread(POP_EINVAL, "tensor %d: rows and cols must be positive", k);
+    if (g[k].dtype != POP_F32 && g[k].dtype != POP_BF16 && g[k].dtype != POP_F16) return fail_thread(POP_EINVAL, "tensor %d: unknown dtype %d", k, g[k].dtype);
+    if ((int64_t)g[k].rows * g[k].cols > kMaxElements) return fail_thread(POP_EUNSUPPORTED, "tensor %d: rows * cols must be at most 2^40", k);
+    pieces += clip_pieces((int64_t)g[k].rows * g[k].cols);
+    if (pieces * P >= kMaxPieces) return fail_thread(POP_EUNSUPPORTED, "gradients of 2^24 or more pieces of 2^13 elements");
+  }
+  return POP_OK;
+}
+
 }  // namespace op
 }  // namespace pop
 
@@ -295,6 +391,116 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
   if ((rc = check_apart(r)) != POP_OK) return rc;
   a.state = state; a.n_slots = n_slots; a.slots = slots;
   return launched(launch_recur_step(a, cfg->dtype, (hipStream_t)hip_stream));
+}
+
+int64_t pop_linear_forward_workspace_bytes(const pop_linear_config* cfg) { return linear_workspace(cfg, false); }
+int64_t pop_linear_backward_workspace_bytes(const pop_linear_config* cfg) { return linear_workspace(cfg, true); }
+
+int pop_linear_forward(const pop_linear_config* cfg, const pop_linear_io* io, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  int rc = linear_common(cfg, io, true);
+  if (rc != POP_OK) return rc;
+  const int64_t need = linear_workspace(cfg, false), states = linear_rows(cfg) * linear_state_bytes(cfg);
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  Regions r = linear_regions(cfg, io, true);
+  r.add("state0", io->state0, states, false, kFirstAndLast);
+  r.add("state_last", io->state_last, states, true, kFirstAndLast);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
+  LinearArgs a = linear_args(cfg, io);
+  a.roles = 1;
+  a.role[0] = {io->q, io->k, io->v, io->o, cfg->key_dim, cfg->value_dim, 0, cfg->scale, 1.0f, io->state0, cfg->value_dim, 1, io->state_last};
+  return launched(launch_linear(a, cfg->dtype, workspace, (hipStream_t)hip_stream));
+}
+
+int pop_linear_backward(const pop_linear_config* cfg, const pop_linear_io* io, const pop_linear_grads* grads,
+                        void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  int rc = linear_common(cfg, io, false);
+  if (rc != POP_OK) return rc;
+  if (!grads) return fail_thread(POP_EINVAL, "grads is NULL");
+  if ((rc = check_floats(grads->dstate_last, "dstate_last", false)) != POP_OK || (rc = check_floats(grads->dstate0, "dstate0", false)) != POP_OK) return rc;
+  const int64_t e = element_bytes(cfg->dtype), K = cfg->key_dim, V = cfg->value_dim;
+  if (cfg->T > 0) {
+    if ((rc = check_heads(cfg, grads->d_o, V, "d_o", false, e)) != POP_OK || (rc = check_heads(cfg, grads->dq, K, "dq", true, e)) != POP_OK ||
+        (rc = check_heads(cfg, grads->dk, K, "dk", true, e)) != POP_OK || (rc = check_heads(cfg, grads->dv, V, "dv", true, e)) != POP_OK)
+      return rc;
+  }
+  const int64_t need = linear_workspace(cfg, true), states = linear_rows(cfg) * linear_state_bytes(cfg);
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  Regions r = linear_regions(cfg, io, false);
+  if (cfg->T > 0) {
+    add_heads(r, cfg, grads->d_o, V, "d_o", e, false);
+    add_heads(r, cfg, grads->dq, K, "dq", e, true);
+    add_heads(r, cfg, grads->dk, K, "dk", e, true);
+    add_heads(r, cfg, grads->dv, V, "dv", e, true);
+  }
+  r.add("state0", io->state0, states, false);
+  r.add("dstate_last", grads->dstate_last, states, false);
+  r.add("dstate0", grads->dstate0, states, true);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
+  // dq_t = scale S_t do_t: the forward pass with do, v, k in the places of q, k, v, its states transposed.  With D the gradient of S_t,
+  // D_t = scale q_t do_t^T + lambda keep_{t+1} D_{t+1}: dv_t = D_t^T k_t and dk_t = D_t v_t, the same from the end.
+  LinearArgs a = linear_args(cfg, io);
+  const float scale = cfg->scale;
+  const int k = (int)K, v = (int)V;
+  a.roles = 3;
+  a.role[0] = {grads->d_o, io->v, io->k, grads->dq, v, k, 0, scale, 1.0f, io->state0, 1, v, nullptr};
+  a.role[1] = {io->k, io->q, grads->d_o, grads->dv, k, v, 1, 1.0f, scale, grads->dstate_last, v, 1, grads->dstate0};
+  a.role[2] = {io->v, grads->d_o, io->q, grads->dk, v, k, 1, 1.0f, scale, grads->dstate_last, 1, v, nullptr};
+  return launched(launch_linear(a, cfg->dtype, workspace, (hipStream_t)hip_stream));
+}
+
+int pop_linear_step(const pop_linear_config* cfg, const pop_linear_io* io, float* state, int32_t n_slots, const int32_t* slots, void* hip_stream) {
+  int rc = check_linear(cfg);
+  if (rc != POP_OK) return rc;
+  if (cfg->T != 1) return fail_thread(POP_EINVAL, "T must be 1 for a single step");
+  if (io && (io->state0 || io->state_last || io->lengths)) return fail_thread(POP_EINVAL, "state0, state_last and lengths must be NULL for a single step");
+  if ((rc = linear_common(cfg, io, true)) != POP_OK || (rc = check_floats(state, "state", true)) != POP_OK || (rc = check_floats(slots, "slots", false)) != POP_OK)
+    return rc;
+  if (n_slots < 1) return fail_thread(POP_EINVAL, "n_slots must be positive");
+  Regions r = linear_regions(cfg, io, true);
+  r.add("slots", slots, (int64_t)cfg->P * cfg->batch * 4, false);
+  if ((__int128)cfg->P * n_slots * cfg->heads * linear_state_bytes(cfg) >> 62) return fail_thread(POP_EUNSUPPORTED, "state has 2^62 bytes or more");
+  r.add("state", state, (int64_t)cfg->P * n_slots * cfg->heads * linear_state_bytes(cfg), true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
+  LinearStep a = {};
+  a.P = cfg->P; a.B = cfg->batch; a.H = cfg->heads; a.K = cfg->key_dim; a.V = cfg->value_dim;
+  a.q = io->q; a.k = io->k; a.v = io->v; a.o = io->o; a.reset = io->reset;
+  a.scale = cfg->scale; a.log_decay = io->log_decay;
+  a.state = state; a.n_slots = n_slots; a.slots = slots;
+  return launched(launch_linear_step(a, cfg->dtype, (hipStream_t)hip_stream));
+}
+
+int64_t pop_clip_workspace_bytes(int32_t P, int32_t n_tensors, const pop_gradient* grads) {
+  const int rc = check_gradients(P, n_tensors, grads);
+  return rc != POP_OK ? rc : clip_workspace_bytes(P, n_tensors, grads);
+}
+
+int pop_clip_gradients(int32_t P, int32_t n_tensors, const pop_gradient* grads, double eps, const float* max_norm, float* norms,
+                       void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  int rc = check_gradients(P, n_tensors, grads);
+  if (rc != POP_OK) return rc;
+  if (!(eps >= 0.0 && eps <= 1e300)) return fail_thread(POP_EINVAL, "eps must be finite and not negative");
+  if ((rc = check_floats(max_norm, "max_norm", false)) != POP_OK || (rc = check_floats(norms, "norms", false)) != POP_OK) return rc;
+  if (!max_norm && !norms) return fail_thread(POP_EINVAL, "max_norm and norms are NULL");
+  ManyRegions<2 * POP_CLIP_MAX_TENSORS + 3> r;
+  for (int k = 0; k < n_tensors; ++k) {
+    const pop_gradient& g = grads[k];
+    const int64_t e = element_bytes(g.dtype);
+    if ((rc = check_matrices(P, g.rows, g.cols, g.grad, "grad", false, e)) != POP_OK) return rc;
+    add_matrices(r, P, g.rows, g.cols, g.grad, "a grad", e, false, k + 1);
+    if (!max_norm) continue;
+    if ((rc = check_matrices(P, g.rows, g.cols, g.out, "out", true, e)) != POP_OK) return rc;
+    add_matrices(r, P, g.rows, g.cols, g.out, "an out", e, true, k + 1);
+  }
+  const int64_t need = clip_workspace_bytes(P, n_tensors, grads);
+  if ((rc = check_workspace(workspace, workspace_bytes, need)) != POP_OK) return rc;
+  r.add("max_norm", max_norm, (int64_t)P * 4, false);
+  r.add("norms", norms, (int64_t)P * 4, true);
+  r.add("workspace", workspace, need, true);
+  if ((rc = check_apart(r)) != POP_OK) return rc;
+  const ClipCall c = {P, n_tensors, grads, eps, max_norm, norms};
+  return launched(launch_clip(c, workspace, (hipStream_t)hip_stream));
 }
 
 int64_t pop_orthogonalize_workspace_bytes(int32_t count, int32_t rows, int32_t cols) {

@@ -1,5 +1,5 @@
 // Operators for populations of recurrent agents: what the boundary (op_api.hip) hands to the launch wrappers of
-// k_recurrence.hip and k_orthogonalize.hip.
+// k_recurrence.hip, k_linear.hip, k_clip.hip and k_orthogonalize.hip.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -36,6 +36,57 @@ int64_t recur_workspace_floats(int64_t P, int64_t B, int64_t T, int64_t C, int64
 hipError_t launch_recur_forward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_backward(const RecurArgs& a, int dtype, hipStream_t s);
 hipError_t launch_recur_step(const RecurArgs& a, int dtype, hipStream_t s);
+
+// ---- linear attention with a decay for each head
+
+// o_t = `read` S_t^T q_t, S_t = lambda keep_t S_{t-1} + `write` k_t v_t^T from `first`.  In reverse time runs from the end and the
+// factor of S lies behind step t instead of in front of it: S_t = lambda keep_{t+1} S_{t+1} + write k_t v_t^T.
+struct LinearRole {
+  pop_heads q, k, v, o;
+  int K, V;                          // widths of q and k, of v and o
+  int reverse;
+  float read, write;
+  const float* first;                // or NULL: zeros.  Element [i, j] of a state at i * first_k + j * first_v
+  int first_k, first_v;
+  float* last;                       // [i, j] at i * V + j; in reverse the gradient in front of step 0; or NULL
+};
+struct LinearArgs {
+  int P, B, T, H;
+  const float* log_decay;            // [P, H] or NULL: zeros
+  pop_sequence reset;
+  const int32_t* lengths;
+  int roles;
+  LinearRole role[3];
+};
+struct LinearStep {
+  int P, B, H, K, V;
+  pop_heads q, k, v, o;              // no step strides
+  pop_sequence reset;
+  float scale;
+  const float* log_decay;
+  float* state;
+  int n_slots;
+  const int32_t* slots;
+};
+int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, int64_t element, bool backward);
+hipError_t launch_linear(const LinearArgs& a, int dtype, void* ws, hipStream_t s);
+hipError_t launch_linear_step(const LinearStep& a, int dtype, hipStream_t s);
+
+
+// ---- norms of gradients, clipping
+
+constexpr int kClipPiece = 1 << 13;  // elements of one agent's part of a tensor that a workgroup takes at a time
+inline int64_t clip_pieces(int64_t elements) { return (elements + kClipPiece - 1) / kClipPiece; }
+
+struct ClipCall {
+  int P, n;
+  const pop_gradient* grads;
+  double eps;
+  const float* max_norm;             // NULL: norms only
+  float* norms;                      // or NULL
+};
+int64_t clip_workspace_bytes(int64_t P, int n, const pop_gradient* grads);
+hipError_t launch_clip(const ClipCall& c, void* ws, hipStream_t s);
 
 
 // ---- orthogonalised updates

@@ -1,21 +1,24 @@
 // Whether the arrays of a call share memory (host only): what the checks of op_api.hip ask of outputs and what lies around them.
 #pragma once
 #include <stdint.h>
+#include <algorithm>
 
 namespace pop {
 
-// Up to three axes of n[i] blocks, stride[i] bytes apart, of `inner` adjacent bytes each.
+constexpr int kAxes = 4;
+
+// Up to kAxes axes of n[i] blocks, stride[i] bytes apart, of `inner` adjacent bytes each.
 struct Region {
   const char* name;
   uintptr_t at;
-  int64_t inner, n[3], stride[3];
+  int64_t inner, n[kAxes], stride[kAxes];
   bool written;
   int same;                          // written over an input of the same nonzero `same` where the two coincide: allowed
   __int128 lo, hi;                   // bytes in front of and behind `at`
 };
 
 inline Region region(const char* name, const void* at, int64_t inner, bool written, int same = 0) {
-  Region r = {name, (uintptr_t)at, inner, {1, 1, 1}, {0, 0, 0}, written, same, 0, inner};
+  Region r = {name, (uintptr_t)at, inner, {1, 1, 1, 1}, {0, 0, 0, 0}, written, same, 0, inner};
   return r;
 }
 inline Region region(const char* name, const void* at, int64_t inner, int axes, const int64_t* n, const int64_t* stride, bool written, int same = 0) {
@@ -37,7 +40,7 @@ class Meeting {
  public:
   Meeting(const Region& a, const Region& b) {
     difference_ = (__int128)b.at - (__int128)a.at;
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < kAxes; ++i) {
       add(a.stride[i], a.n[i] - 1);
       add(-(__int128)b.stride[i], b.n[i] - 1);
     }
@@ -79,14 +82,14 @@ class Meeting {
     }
     return false;
   }
-  Term term_[6];
-  __int128 lo_[7], hi_[7], difference_;
+  Term term_[2 * kAxes];
+  __int128 lo_[2 * kAxes + 1], hi_[2 * kAxes + 1], difference_;
   int count_ = 0, looked_ = 0;
 };
 
 inline bool coincide(const Region& a, const Region& b) {
   bool same = a.at == b.at && a.inner == b.inner;
-  for (int i = 0; i < 3; ++i) same = same && a.n[i] == b.n[i] && a.stride[i] == b.stride[i];
+  for (int i = 0; i < kAxes; ++i) same = same && a.n[i] == b.n[i] && a.stride[i] == b.stride[i];
   return same;
 }
 inline bool meet(const Region& a, const Region& b) {
@@ -116,6 +119,34 @@ class Regions {
  private:
   Region region_[32];                // three arrays of eight layers, hyperparameters, workspace
   int count_ = 0;
+};
+
+// The same for calls of up to N arrays: sorted by where they begin, so that each is compared with those that begin within it only.
+template <int N> class ManyRegions {
+ public:
+  template <typename... A> void add(const char* name, const void* at, int64_t inner, A... rest) {
+    if (at && inner > 0) region_[count_++] = region(name, at, inner, rest...);
+  }
+  bool clash(const char*& one, const char*& other) {
+    for (int i = 0; i < count_; ++i) order_[i] = i;
+    std::sort(order_, order_ + count_, [this](int a, int b) { return first(a) < first(b); });
+    for (int i = 0; i < count_; ++i) {
+      const Region& a = region_[order_[i]];
+      for (int k = i + 1; k < count_ && first(order_[k]) < (__int128)a.at + a.hi; ++k) {
+        const Region& b = region_[order_[k]];
+        if ((!a.written && !b.written) || !meet(a, b) || (a.same && a.same == b.same && coincide(a, b))) continue;
+        one = a.name;
+        other = b.name;
+        return true;
+      }
+    }
+    return false;
+  }
+
+ private:
+  __int128 first(int i) const { return (__int128)region_[i].at + region_[i].lo; }
+  Region region_[N];
+  int order_[N], count_ = 0;
 };
 
 }  // namespace pop

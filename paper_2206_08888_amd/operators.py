@@ -1,5 +1,5 @@
-"""Operators for populations of recurrent agents on device tensors: the gated linear recurrence and the orthogonalised
-(Muon) update.  Argument marshalling for the calls of include/pop.h of the same names; everything is computed in the
+"""Operators for populations of recurrent agents on device tensors: the gated linear recurrence, linear attention with a decay
+for each head, clipping of gradients by their norm, and the orthogonalised (Muon) update.  Argument marshalling for the calls of include/pop.h of the same names; everything is computed in the
 HIP kernels of libpop.so, on PyTorch's current stream, asynchronously.
 
 Outputs and workspaces come from PyTorch's allocator, call by call, so calls may run on any stream and inside
@@ -15,8 +15,8 @@ import torch
 from torch.autograd.graph import increment_version
 
 from .binding import (  # noqa: F401
-    MUON_MAX_LAYERS, NS_COEF, NS_MAX_STEPS, POP_BF16, POP_F16, POP_F32, _check, load_library, make_ns_config, pop_matrices,
-    pop_muon_layer, pop_ns_config,
+    CLIP_MAX_TENSORS, MUON_MAX_LAYERS, NS_COEF, NS_MAX_STEPS, POP_BF16, POP_F16, POP_F32, _check, load_library, make_ns_config,
+    pop_gradient, pop_heads, pop_linear_config, pop_linear_grads, pop_linear_io, pop_matrices, pop_muon_layer, pop_ns_config,
     pop_recurrence_config, pop_recurrence_grads, pop_recurrence_io, pop_sequence,
 )
 
@@ -77,6 +77,24 @@ class _Operator:
     def _pointer(self, t, name, shape, dtype=torch.float32):
         return None if t is None else self._tensor(t, name, shape, dtype).data_ptr()
 
+    def _reset(self, reset, shape):
+        if reset is None:
+            return None, 0, 0, 0
+        dtype = torch.bool if getattr(reset, "dtype", None) is torch.bool else torch.uint8
+        s = self._tensor(reset, "reset", shape, dtype, contiguous=False).stride()
+        return reset.data_ptr(), s[0], s[1], s[2] if len(s) == 3 else 0
+
+    def _state_table(self, state, axes, slots):
+        """The number of slots of a table with as many axes as the text `axes` names."""
+        if not isinstance(state, torch.Tensor) or state.dim() != axes.count(",") + 1:
+            raise ValueError("state must be a [%s] tensor" % axes)
+        n_slots = state.shape[1]
+        if n_slots >> 31:
+            _sizes(n_slots)
+        if slots is None and n_slots < self.batch:
+            raise ValueError("state has %d rows for %d sequences and no slots are given" % (n_slots, self.batch))
+        return n_slots
+
     def _empty(self, shape, dtype=None):
         return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
 
@@ -115,13 +133,6 @@ class Recurrence(_Operator):
         if s[-1] != 1 and self.C > 1:
             raise ValueError("%s: its channels must be adjacent" % name)
         return t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0
-
-    def _reset(self, reset, shape):
-        if reset is None:
-            return None, 0, 0, 0
-        dtype = torch.bool if getattr(reset, "dtype", None) is torch.bool else torch.uint8
-        s = self._tensor(reset, "reset", shape, dtype, contiguous=False).stride()
-        return reset.data_ptr(), s[0], s[1], s[2] if len(s) == 3 else 0
 
     def _io(self, x, g, bias, h0, reset, lengths):
         T = x.shape[2] if x.dim() == 4 else -1
@@ -168,13 +179,7 @@ class Recurrence(_Operator):
         [P, batch] int32 names each row's state (none twice within an agent); a row whose slot is negative or not
         below n_slots is idle and gets zeros.  Without slots row b has state b."""
         shape = self._rows
-        if not isinstance(state, torch.Tensor) or state.dim() != 3:
-            raise ValueError("state must be a [P, n_slots, C] tensor")
-        n_slots = state.shape[1]
-        if n_slots >> 31:
-            _sizes(n_slots)
-        if slots is None and n_slots < self.batch:
-            raise ValueError("state has %d rows for %d sequences and no slots are given" % (n_slots, self.batch))
+        n_slots = self._state_table(state, "P, n_slots, C", slots)
         xs, gs = self._sequence(x, "x", shape), self._sequence(g, "g", shape)
         y = x.new_empty(shape)
         io = pop_recurrence_io(xs, gs, (y.data_ptr(), self.batch * self.C, self.C, 0), self._reset(reset, shape[:2]),
@@ -185,7 +190,89 @@ class Recurrence(_Operator):
         return y
 
 
-class _NewtonSchulz(_Operator):
+class LinearAttention(_Operator):
+    """A matrix for a memory: S_t = exp(log_decay) S_{t-1} + k_t v_t^T and o_t = scale S_t^T q_t, for P agents with `batch`
+    sequences of up to T steps and `heads` heads each; where `reset` is not zero the state in front of that step counts as zero.
+
+    q, k [P, batch, T', heads, key_dim], v, o [P, batch, T', heads, value_dim] and their gradients are of `dtype`, T' <= T, any
+    strides with adjacent channels; both widths at most 128.  log_decay [P, heads] (at most 0; None: nothing decays) and the states
+    state0, state_last, dstate_last, dstate0 [P, batch, heads, key_dim, value_dim] are float32; reset and lengths as in Recurrence.
+    scale: by default key_dim ** -0.5."""
+
+    def __init__(self, P, batch, T, heads, key_dim, value_dim, dtype=torch.float32, device="cuda", scale=None):
+        super().__init__(dtype, device)
+        _sizes(P, batch, T, heads, key_dim, value_dim)
+        self.P, self.batch, self.T, self.heads, self.key_dim, self.value_dim = P, batch, T, heads, key_dim, value_dim
+        self.scale = max(1, key_dim) ** -0.5 if scale is None else float(scale)
+        self._decays, self._states = (P, heads), (P, batch, heads, key_dim, value_dim)
+        _check(self.lib.pop_linear_forward_workspace_bytes(ct.byref(self._config(T))))
+        self._one = self._config(1)
+        self._one_ref = ct.byref(self._one)
+        self._bytes = {}
+
+    def _config(self, T):
+        return pop_linear_config(self.P, self.batch, T, self.heads, self.key_dim, self.value_dim, self.code, self.scale)
+
+    def _heads(self, t, name, shape):
+        """The fields of a pop_heads of [P, batch, T, heads, width], or [P, batch, heads, width] for single steps."""
+        s = self._tensor(t, name, shape, contiguous=False).stride()
+        if s[-1] != 1 and shape[-1] > 1:
+            raise ValueError("%s: its channels must be adjacent" % name)
+        return (t.data_ptr(), s[0], s[1], s[2], s[3]) if len(s) == 5 else (t.data_ptr(), s[0], s[1], 0, s[2])
+
+    def _io(self, q, k, v, log_decay, state0, reset, lengths):
+        T = q.shape[2] if q.dim() == 5 else -1
+        if T < 0 or T > self.T:
+            raise ValueError("q must have shape [%d, %d, up to %d, %d, %d], not %s"
+                             % (self.P, self.batch, self.T, self.heads, self.key_dim, tuple(q.shape)))
+        keys, values = (self.P, self.batch, T, self.heads, self.key_dim), (self.P, self.batch, T, self.heads, self.value_dim)
+        io = pop_linear_io(self._heads(q, "q", keys), self._heads(k, "k", keys), self._heads(v, "v", values), (None, 0, 0, 0, 0),
+                           self._reset(reset, keys[:3]), self._pointer(log_decay, "log_decay", self._decays),
+                           self._pointer(state0, "state0", self._states), None, self._pointer(lengths, "lengths", keys[:2], torch.int32))
+        return self._config(T), io, keys, values
+
+    def _workspace(self, sizes, cfg):
+        n = self._bytes.get((sizes, cfg.T))
+        if n is None:
+            n = self._bytes[sizes, cfg.T] = _check(getattr(self.lib, sizes)(ct.byref(cfg)))
+        return self._empty(n, torch.uint8), n
+
+    def forward(self, q, k, v, log_decay=None, state0=None, reset=None, lengths=None):
+        """(o, state_last)"""
+        cfg, io, _, values = self._io(q, k, v, log_decay, state0, reset, lengths)
+        o, last = self._empty(values), self._empty(self._states, torch.float32)
+        io.o, io.state_last = self._heads(o, "o", values), last.data_ptr()
+        ws, n = self._workspace("pop_linear_forward_workspace_bytes", cfg)
+        self._call(self.lib.pop_linear_forward, ct.byref(cfg), ct.byref(io), ws.data_ptr(), n)
+        return o, last
+
+    def backward(self, q, k, v, do, log_decay=None, state0=None, reset=None, lengths=None, dstate_last=None):
+        """(dq, dk, dv, dstate0) of sum(o do) + sum(state_last dstate_last), from what `forward` was given."""
+        cfg, io, keys, values = self._io(q, k, v, log_decay, state0, reset, lengths)
+        dq, dk, dv, dstate0 = self._empty(keys), self._empty(keys), self._empty(values), self._empty(self._states, torch.float32)
+        grads = pop_linear_grads(self._heads(do, "do", values), self._heads(dq, "dq", keys), self._heads(dk, "dk", keys),
+                                 self._heads(dv, "dv", values), self._pointer(dstate_last, "dstate_last", self._states), dstate0.data_ptr())
+        ws, n = self._workspace("pop_linear_backward_workspace_bytes", cfg)
+        self._call(self.lib.pop_linear_backward, ct.byref(cfg), ct.byref(io), ct.byref(grads), ws.data_ptr(), n)
+        return dq, dk, dv, dstate0
+
+    def step(self, q, k, v, state, log_decay=None, reset=None, slots=None):
+        """One step of acting agents: q, k [P, batch, heads, key_dim], v, o [P, batch, heads, value_dim]; state [P, n_slots, heads,
+        key_dim, value_dim] float32 is updated in place.  slots as in Recurrence.step."""
+        n_slots = self._state_table(state, "P, n_slots, heads, key_dim, value_dim", slots)
+        rows = (self.P, self.batch)
+        keys, values = (*rows, self.heads, self.key_dim), (*rows, self.heads, self.value_dim)
+        qs, ks, vs = self._heads(q, "q", keys), self._heads(k, "k", keys), self._heads(v, "v", values)
+        o = v.new_empty(values)
+        io = pop_linear_io(qs, ks, vs, (o.data_ptr(), self.batch * self.heads * self.value_dim, self.heads * self.value_dim, 0, self.value_dim),
+                           self._reset(reset, rows), self._pointer(log_decay, "log_decay", self._decays))
+        self._call(self.lib.pop_linear_step, self._one_ref, ct.byref(io), self._pointer(state, "state", (self.P, n_slots, *self._states[2:])),
+                   n_slots, self._pointer(slots, "slots", rows, torch.int32))
+        increment_version(state)
+        return o
+
+
+class _Stacks(_Operator):
     def _matrices(self, t, name, shape, dtype=None):
         t = self._tensor(t, name, shape, dtype, contiguous=False)
         s = t.stride()
@@ -194,7 +281,7 @@ class _NewtonSchulz(_Operator):
         return pop_matrices(t.data_ptr(), s[0], s[1])
 
 
-class Orthogonalizer(_NewtonSchulz):
+class Orthogonalizer(_Stacks):
     """orthogonalizer(g): Newton-Schulz products drive the singular values of every matrix of g [count, rows, cols]
     towards 1 (the products an orthogonalised optimiser takes its updates through).  Any strides with adjacent columns."""
 
@@ -217,7 +304,7 @@ class Orthogonalizer(_NewtonSchulz):
         return out
 
 
-class Muon(_NewtonSchulz):
+class Muon(_Stacks):
     """One optimiser step for the weight matrices of P agents, layer by layer [P, rows, cols]:
 
       M = mu M + G;  U = G + mu M (nesterov) or M;  W = (1 - lr wd) W - lr scale O,  O = U orthogonalised
@@ -255,3 +342,66 @@ class Muon(_NewtonSchulz):
         self._call(self.lib.pop_muon_step, ct.byref(self._ns), self.P, len(self.shapes), layers, self.code, int(self.nesterov),
                    self._pointer(hparams, "hparams", (self.P, 3)), ws.data_ptr(), self._bytes)
         increment_version([*weights, *momenta])
+
+
+class GradientClip(_Stacks):
+    """clip(grads, max_norm): the norm of every agent's gradients over all tensors of the list, and the gradients scaled down where
+    it is above the agent's limit:
+
+      norm_i = sqrt(sum g^2);  out = g where norm_i + eps <= max_norm_i, else g max_norm_i / (norm_i + eps)
+
+    shapes: of each tensor (at most 256) behind the agents' axis, e.g. (17, 256), (256,); tensors of three axes or fewer may have any
+    strides with an adjacent last one, an agent's part of others lies in one piece.  dtype: one for all, or a list."""
+
+    def __init__(self, P, shapes, dtype=torch.float32, device="cuda", eps=1e-6):
+        dtypes = list(dtype) if isinstance(dtype, (list, tuple)) else [dtype] * len(shapes)
+        super().__init__(dtypes[0] if dtypes else dtype, device)
+        self.P, self.eps, self.shapes, self.dtypes = P, float(eps), [(P, *s) for s in shapes], dtypes
+        if len(dtypes) != len(self.shapes):
+            raise ValueError("%d types for %d tensors" % (len(dtypes), len(self.shapes)))
+        self._layout = (pop_gradient * max(1, len(self.shapes)))()
+        for g, shape, dt in zip(self._layout, self.shapes, dtypes):
+            rows = 1
+            for v in shape[1:-1]:
+                rows *= v
+            _sizes(*shape, rows)
+            g.rows, g.cols, g.dtype = rows, shape[-1] if len(shape) > 1 else 1, _dtype_code(dt)
+        self._bytes = _check(self.lib.pop_clip_workspace_bytes(P, len(self.shapes), self._layout))
+
+    def _list(self, tensors, name):
+        if len(tensors) != len(self.shapes):
+            raise ValueError("%s must have %d tensors, not %d" % (name, len(self.shapes), len(tensors)))
+        for t, shape, dt in zip(tensors, self.shapes, self.dtypes):
+            s = self._tensor(t, name, shape, dt, contiguous=False).stride()
+            if len(s) <= 3:
+                if len(s) > 1 and s[-1] != 1 and shape[-1] > 1:
+                    raise ValueError("%s: its last axis must be adjacent" % name)
+                yield t.data_ptr(), s[0], s[1] if len(s) == 3 else 0
+            else:
+                if not t[0].is_contiguous():
+                    raise ValueError("%s: an agent's part of a tensor of %d axes must be contiguous" % (name, len(s)))
+                yield t.data_ptr(), s[0], shape[-1]
+
+    def _run(self, grads, outs, max_norm):
+        layout = type(self._layout).from_buffer_copy(self._layout)
+        for g, m in zip(layout, self._list(grads, "grads")):
+            g.grad = m
+        if outs is not None:
+            for g, m in zip(layout, self._list(outs, "out")):
+                g.out = m
+        norms, ws = self._empty(self.P, torch.float32), self._empty(self._bytes, torch.uint8)
+        self._call(self.lib.pop_clip_gradients, self.P, len(self.shapes), layout, self.eps, max_norm, norms.data_ptr(), ws.data_ptr(), self._bytes)
+        return norms
+
+    def __call__(self, grads, max_norm, out=None):
+        """(clipped, norms): new tensors, or those of the list `out` (which may be grads, with the same strides).  max_norm: float32
+        tensor [P] on the device.  norms [P]: float32, before clipping."""
+        outs = [self._empty(s, dt) for s, dt in zip(self.shapes, self.dtypes)] if out is None else out
+        norms = self._run(grads, outs, self._tensor(max_norm, "max_norm", (self.P,), torch.float32).data_ptr())
+        if out is not None:
+            increment_version(list(out))
+        return outs, norms
+
+    def norms(self, grads):
+        """The norms alone: float32 [P]."""
+        return self._run(grads, None, None)
