@@ -11,7 +11,10 @@ namespace pop {
 namespace {
 namespace clip {
 
-constexpr int kThreads = 256, kTensors = 32;
+constexpr int kThreads = 256;
+constexpr int kFew = kThreads;         // sums of pieces that a workgroup reads at once
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 struct Tensor {
   const void* in;
@@ -19,10 +22,11 @@ struct Tensor {
   int64_t in_matrix, in_row, out_matrix, out_row, elements;
   int cols, dtype;                   // cols 0: an agent's part lies in one piece
   int first;                         // piece of the launch
+  int wide;                          // vectors of 16 bytes end where rows end
 };
-struct Tensors {
+template <int N> struct Tensors {
   int n, pieces;
-  Tensor t[kTensors];
+  Tensor t[N];
 };
 
 __device__ inline double sum_of_wave(double v) {
@@ -38,67 +42,157 @@ __device__ inline double sum_of_group(double v, double* part) {
   return part[0] + part[1] + part[2] + part[3];
 }
 
-struct Place { int agent, tensor; int64_t from; };
-__device__ inline Place place_of(const Tensors& a) {
+struct Place { int agent, tensor, count; int64_t from; };
+template <int N> __device__ inline Place place_of(const Tensors<N>& a, int block) {
   Place p;
-  p.agent = blockIdx.x / a.pieces;
-  const int piece = blockIdx.x - p.agent * a.pieces;
+  p.agent = block / a.pieces;
+  const int piece = block - p.agent * a.pieces;
   p.tensor = 0;
   while (p.tensor + 1 < a.n && a.t[p.tensor + 1].first <= piece) ++p.tensor;
   p.from = (int64_t)(piece - a.t[p.tensor].first) * kClipPiece;
+  const int64_t left = a.t[p.tensor].elements - p.from;
+  p.count = left < kClipPiece ? (int)left : kClipPiece;
   return p;
 }
-__device__ inline int64_t offset(int64_t e, int cols, int64_t row) {
-  if (cols == 0) return e;
-  const int64_t r = e / cols;
-  return r * row + (e - r * cols);
-}
+
+// Where the elements of a piece lie: element i at `at`(i) from the agent's part.
+struct Rows {
+  int64_t row, first;
+  unsigned cols, skip;
+  __device__ inline Rows(int64_t from, int cols, int64_t row) : row(row), first(from), cols(cols), skip(0) {
+    if (cols != 0) {
+      first = from / cols;
+      skip = (unsigned)(from - first * cols);
+    }
+  }
+  __device__ inline int64_t at(int i) const {
+    if (cols == 0) return first + i;
+    const unsigned r = (skip + i) / cols;                            // skip < 2^31, i < 2^13
+    return (first + r) * row + (skip + i - r * cols);
+  }
+};
+
+// What a thread has of a piece: vectors of 16 bytes threadIdx.x, threadIdx.x + kThreads, ..; where rows do not allow them, and behind the
+// last whole one, the vector's elements one by one.  Vectors need no more alignment than elements.
+template <typename E> struct Part {
+  static constexpr int kVec = 16 / sizeof(E), kEach = kClipPiece / kVec / kThreads;
+  u32x4 v[kEach];
+  static __device__ inline int at(int k) { return (int)(threadIdx.x + k * kThreads) * kVec; }
+  __device__ inline void load(const E* in, const Rows& rows, int count, bool wide) {
+    if (wide && count == kClipPiece) {
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) __builtin_memcpy(&v[k], in + rows.at(at(k)), 16);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        v[k] = u32x4{0, 0, 0, 0};
+        if (wide && at(k) + kVec <= count) {
+          __builtin_memcpy(&v[k], in + rows.at(at(k)), 16);
+        } else {
+          E e[kVec];
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) e[i] = at(k) + i < count ? in[rows.at(at(k) + i)] : (E)0.0f;
+          __builtin_memcpy(&v[k], e, 16);
+        }
+      }
+    }
+  }
+  __device__ inline void store(E* out, const Rows& rows, int count, bool wide) const {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (wide && at(k) + kVec <= count) {
+        __builtin_memcpy(out + rows.at(at(k)), &v[k], 16);
+      } else {
+        E e[kVec];
+        __builtin_memcpy(e, &v[k], 16);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (at(k) + i < count) out[rows.at(at(k) + i)] = e[i];
+      }
+    }
+  }
+};
 
 template <typename E> __device__ inline double squares(const Tensor& t, const Place& p) {
-  const E* in = (const E*)t.in + p.agent * t.in_matrix;
+  Part<E> part;
+  part.load((const E*)t.in + p.agent * t.in_matrix, Rows(p.from, t.cols, t.in_row), p.count, t.wide);
   double s = 0.0;
-  for (int i = threadIdx.x; i < kClipPiece; i += kThreads) {
-    if (p.from + i >= t.elements) break;
-    const double v = (double)(float)in[offset(p.from + i, t.cols, t.in_row)];
-    s = fma(v, v, s);
+#pragma unroll
+  for (int k = 0; k < Part<E>::kEach; ++k) {
+    E e[Part<E>::kVec];
+    __builtin_memcpy(e, &part.v[k], 16);
+#pragma unroll
+    for (int i = 0; i < Part<E>::kVec; ++i) {
+      const double v = (double)(float)e[i];
+      s = fma(v, v, s);
+    }
   }
   return s;
 }
-__global__ void __launch_bounds__(kThreads) k_squares(Tensors a, double* sums, int pieces_of_all, int first) {
+template <int N> __global__ void __launch_bounds__(kThreads) k_squares(Tensors<N> a, double* sums, int pieces_of_all, int first) {
   __shared__ double part[4];
-  const Place p = place_of(a);
+  const Place p = place_of(a, blockIdx.x);
   const Tensor& t = a.t[p.tensor];
   const double s = t.dtype == POP_F32 ? squares<float>(t, p) : t.dtype == POP_BF16 ? squares<__bf16>(t, p) : squares<_Float16>(t, p);
   const double all = sum_of_group(s, part);
-  if (threadIdx.x == 0) sums[(int64_t)p.agent * pieces_of_all + first + blockIdx.x % a.pieces] = all;
+  if (threadIdx.x == 0) sums[(int64_t)p.agent * pieces_of_all + first + (int)blockIdx.x - p.agent * a.pieces] = all;
 }
 
-__global__ void __launch_bounds__(kThreads) k_norms(const double* sums, int pieces, double eps, const float* max_norm, float* norms, float* factor) {
-  __shared__ double part[4];
+struct Limits {
+  const double* sums;
+  int pieces;
+  double eps;
+  const float* max_norm;
+  float* norms;
+};
+__device__ inline double norm_of(const Limits& l, int agent, double* part) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < pieces; i += kThreads) s += sums[(int64_t)blockIdx.x * pieces + i];
-  s = sum_of_group(s, part);
+  for (int i = threadIdx.x; i < l.pieces; i += kThreads) s += l.sums[(int64_t)agent * l.pieces + i];
+  return sqrt(sum_of_group(s, part));
+}
+__device__ inline float factor_of(const Limits& l, int agent, double norm) {
+  const float m = l.max_norm[agent];
+  const double limit = m < 0.0f ? 0.0 : (double)m, above = norm + l.eps;
+  return above <= limit ? 1.0f : (float)(limit / above);
+}
+__global__ void __launch_bounds__(kThreads) k_norms(Limits l, float* factor) {
+  __shared__ double part[4];
+  const double norm = norm_of(l, blockIdx.x, part);
   if (threadIdx.x != 0) return;
-  const double norm = sqrt(s), above = norm + eps;
-  if (norms) norms[blockIdx.x] = (float)norm;
-  if (!max_norm) return;
-  const float m = max_norm[blockIdx.x];
-  const double limit = m < 0.0f ? 0.0 : (double)m;
-  factor[blockIdx.x] = above <= limit ? 1.0f : (float)(limit / above);
+  if (l.norms) l.norms[blockIdx.x] = (float)norm;
+  if (factor) factor[blockIdx.x] = factor_of(l, blockIdx.x, norm);
 }
 
 template <typename E> __device__ inline void scale(const Tensor& t, const Place& p, float f) {
   const E* in = (const E*)t.in + p.agent * t.in_matrix;
   E* out = (E*)t.out + p.agent * t.out_matrix;
-  for (int i = threadIdx.x; i < kClipPiece; i += kThreads) {
-    if (p.from + i >= t.elements) break;
-    out[offset(p.from + i, t.cols, t.out_row)] = (E)((float)in[offset(p.from + i, t.cols, t.in_row)] * f);
+  if (f == 1.0f && in == out) return;                                // (the boundary has checked that strides are the same then)
+  Part<E> part;
+  part.load(in, Rows(p.from, t.cols, t.in_row), p.count, t.wide);
+#pragma unroll
+  for (int k = 0; k < Part<E>::kEach; ++k) {
+    E e[Part<E>::kVec];
+    __builtin_memcpy(e, &part.v[k], 16);
+#pragma unroll
+    for (int i = 0; i < Part<E>::kVec; ++i) e[i] = (E)((float)e[i] * f);
+    __builtin_memcpy(&part.v[k], e, 16);
   }
+  part.store(out, Rows(p.from, t.cols, t.out_row), p.count, t.wide);
 }
-__global__ void __launch_bounds__(kThreads) k_scale(Tensors a, const float* factor) {
-  const Place p = place_of(a);
+// factor NULL: every workgroup finds its agent's norm for itself, and the one with the agent's first piece of all writes it.
+template <int N> __global__ void __launch_bounds__(kThreads) k_scale(Tensors<N> a, Limits l, const float* factor, int first) {
+  __shared__ double part[4];
+  const int block = gridDim.x - 1 - blockIdx.x;                      // what was read last may still be in a cache
+  const Place p = place_of(a, block);
   const Tensor& t = a.t[p.tensor];
-  const float f = factor[p.agent];
+  float f;
+  if (factor) {
+    f = factor[p.agent];
+  } else {
+    const double norm = norm_of(l, p.agent, part);
+    f = factor_of(l, p.agent, norm);
+    if (l.norms && threadIdx.x == 0 && first == 0 && block == p.agent * a.pieces) l.norms[p.agent] = (float)norm;
+  }
   if (t.dtype == POP_F32) scale<float>(t, p, f);
   else if (t.dtype == POP_BF16) scale<__bf16>(t, p, f);
   else scale<_Float16>(t, p, f);
@@ -110,9 +204,10 @@ int64_t all_pieces(int n, const pop_gradient* g) {
   return sum;
 }
 
-Tensors tensors_of(const ClipCall& c, int from, int to) {
-  Tensors a = {};
-  for (int k = from; k < to; ++k) {
+template <int N> Tensors<N> tensors_of(const ClipCall& c, int from) {
+  Tensors<N> a;
+  a.n = a.pieces = 0;
+  for (int k = from; k < c.n && k < from + N; ++k) {
     const pop_gradient& g = c.grads[k];
     Tensor& t = a.t[a.n++];
     t.in = g.grad.data; t.in_matrix = g.grad.matrix; t.in_row = g.grad.row;
@@ -120,10 +215,30 @@ Tensors tensors_of(const ClipCall& c, int from, int to) {
     t.elements = (int64_t)g.rows * g.cols;
     t.cols = g.rows == 1 || (g.grad.row == g.cols && (!c.max_norm || g.out.row == g.cols)) ? 0 : g.cols;
     t.dtype = g.dtype;
+    t.wide = t.cols % (g.dtype == POP_F32 ? 4 : 8) == 0;
     t.first = a.pieces;
     a.pieces += (int)clip_pieces(t.elements);
   }
   return a;
+}
+
+template <int N> void launch(const ClipCall& c, const Limits& l, float* factor, hipStream_t s) {
+  const bool few = c.max_norm && l.pieces <= kFew;
+  int first = 0;
+  Tensors<N> a;
+  for (int k = 0; k < c.n; k += N) {
+    a = tensors_of<N>(c, k);
+    k_squares<N><<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, (double*)l.sums, l.pieces, first);
+    first += a.pieces;
+  }
+  if (!few) k_norms<<<(unsigned)c.P, kThreads, 0, s>>>(l, c.max_norm ? factor : nullptr);
+  if (!c.max_norm) return;
+  first = 0;
+  for (int k = 0; k < c.n; k += N) {
+    if (c.n > N) a = tensors_of<N>(c, k);
+    k_scale<N><<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, l, few ? nullptr : factor, first);
+    first += a.pieces;
+  }
 }
 
 }  // namespace clip
@@ -138,18 +253,9 @@ hipError_t launch_clip(const ClipCall& c, void* ws, hipStream_t s) {
   const int pieces = (int)all_pieces(c.n, c.grads);
   double* sums = (double*)ws;
   float* factor = (float*)(sums + (int64_t)c.P * pieces);
-  int first = 0;
-  for (int k = 0; k < c.n; k += kTensors) {
-    const Tensors a = tensors_of(c, k, k + kTensors < c.n ? k + kTensors : c.n);
-    k_squares<<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, sums, pieces, first);
-    first += a.pieces;
-  }
-  k_norms<<<(unsigned)c.P, kThreads, 0, s>>>(sums, pieces, c.eps, c.max_norm, c.norms, factor);
-  if (c.max_norm)
-    for (int k = 0; k < c.n; k += kTensors) {
-      const Tensors a = tensors_of(c, k, k + kTensors < c.n ? k + kTensors : c.n);
-      k_scale<<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, factor);
-    }
+  const Limits l = {sums, pieces, c.eps, c.max_norm, c.norms};
+  if (c.n <= 8) clip::launch<8>(c, l, factor, s);
+  else clip::launch<32>(c, l, factor, s);
   return hipGetLastError();
 }
 

@@ -10,6 +10,7 @@ gradients are recorded (pass them detached, or under torch.no_grad()); Muon, as 
 graph.  Tensors that are written in place raise their version, so that graphs which kept them notice.
 """
 import ctypes as ct
+import struct
 
 import torch
 from torch.autograd.graph import increment_version
@@ -367,41 +368,51 @@ class GradientClip(_Stacks):
             _sizes(*shape, rows)
             g.rows, g.cols, g.dtype = rows, shape[-1] if len(shape) > 1 else 1, _dtype_code(dt)
         self._bytes = _check(self.lib.pop_clip_workspace_bytes(P, len(self.shapes), self._layout))
+        self._agents, self._call_layout = (P,), type(self._layout)
+        self._words = [struct.unpack("2q", bytes(g)[:16]) for g in self._layout]
+        self._strides = [(g.rows * g.cols, g.cols) for g in self._layout]      # of new tensors
+        self._no_outs = [(0, 0, 0)] * len(self.shapes)
+        self._pack = struct.Struct("%dq" % (8 * len(self.shapes))).pack
 
     def _list(self, tensors, name):
+        """The fields of a pop_matrices for each of them."""
         if len(tensors) != len(self.shapes):
             raise ValueError("%s must have %d tensors, not %d" % (name, len(self.shapes), len(tensors)))
+        fields = []
         for t, shape, dt in zip(tensors, self.shapes, self.dtypes):
             s = self._tensor(t, name, shape, dt, contiguous=False).stride()
             if len(s) <= 3:
                 if len(s) > 1 and s[-1] != 1 and shape[-1] > 1:
                     raise ValueError("%s: its last axis must be adjacent" % name)
-                yield t.data_ptr(), s[0], s[1] if len(s) == 3 else 0
+                fields.append((t.data_ptr(), s[0], s[1] if len(s) == 3 else 0))
             else:
                 if not t[0].is_contiguous():
                     raise ValueError("%s: an agent's part of a tensor of %d axes must be contiguous" % (name, len(s)))
-                yield t.data_ptr(), s[0], shape[-1]
+                fields.append((t.data_ptr(), s[0], shape[-1]))
+        return fields
 
     def _run(self, grads, outs, max_norm):
-        layout = type(self._layout).from_buffer_copy(self._layout)
-        for g, m in zip(layout, self._list(grads, "grads")):
-            g.grad = m
-        if outs is not None:
-            for g, m in zip(layout, self._list(outs, "out")):
-                g.out = m
-        norms, ws = self._empty(self.P, torch.float32), self._empty(self._bytes, torch.uint8)
+        words = []                                       # the structures as words of 64 bits, the quickest way to fill them
+        for layout, g, o in zip(self._words, self._list(grads, "grads"), outs):
+            words += layout
+            words += g
+            words += o
+        layout = self._call_layout.from_buffer_copy(self._pack(*words))
+        norms, ws = self._empty(self._agents, torch.float32), self._empty(self._bytes, torch.uint8)
         self._call(self.lib.pop_clip_gradients, self.P, len(self.shapes), layout, self.eps, max_norm, norms.data_ptr(), ws.data_ptr(), self._bytes)
         return norms
 
     def __call__(self, grads, max_norm, out=None):
         """(clipped, norms): new tensors, or those of the list `out` (which may be grads, with the same strides).  max_norm: float32
         tensor [P] on the device.  norms [P]: float32, before clipping."""
-        outs = [self._empty(s, dt) for s, dt in zip(self.shapes, self.dtypes)] if out is None else out
-        norms = self._run(grads, outs, self._tensor(max_norm, "max_norm", (self.P,), torch.float32).data_ptr())
+        limits = self._tensor(max_norm, "max_norm", self._agents, torch.float32).data_ptr()
         if out is not None:
+            norms = self._run(grads, self._list(out, "out"), limits)
             increment_version(list(out))
-        return outs, norms
+            return out, norms
+        out = [torch.empty(s, dtype=dt, device=self.device) for s, dt in zip(self.shapes, self.dtypes)]
+        return out, self._run(grads, [(t.data_ptr(), *s) for t, s in zip(out, self._strides)], limits)
 
     def norms(self, grads):
         """The norms alone: float32 [P]."""
-        return self._run(grads, None, None)
+        return self._run(grads, self._no_outs, None)
