@@ -14,6 +14,9 @@ namespace clip {
 constexpr int kThreads = 256;
 constexpr int kFew = kThreads;         // sums of pieces that a workgroup reads at once
 
+// Pieces from which on results are stored past the caches, which hold what is about to be read again: a quarter of the 256 MB of the last one.
+constexpr int kPast = (64 << 20) / (4 * kClipPiece);
+
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 struct Tensor {
@@ -97,11 +100,14 @@ template <typename E> struct Part {
       }
     }
   }
-  __device__ inline void store(E* out, const Rows& rows, int count, bool wide) const {
+  template <bool PAST> __device__ inline void store(E* out, const Rows& rows, int count, bool wide) const {
+    typedef u32x4 Anywhere __attribute__((aligned(2)));
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       if (wide && at(k) + kVec <= count) {
-        __builtin_memcpy(out + rows.at(at(k)), &v[k], 16);
+        Anywhere* to = (Anywhere*)(out + rows.at(at(k)));
+        if constexpr (PAST) __builtin_nontemporal_store(v[k], to);
+        else *to = v[k];
       } else {
         E e[kVec];
         __builtin_memcpy(e, &v[k], 16);
@@ -163,7 +169,7 @@ __global__ void __launch_bounds__(kThreads) k_norms(Limits l, float* factor) {
   if (factor) factor[blockIdx.x] = factor_of(l, blockIdx.x, norm);
 }
 
-template <typename E> __device__ inline void scale(const Tensor& t, const Place& p, float f) {
+template <typename E, bool PAST> __device__ inline void scale(const Tensor& t, const Place& p, float f) {
   const E* in = (const E*)t.in + p.agent * t.in_matrix;
   E* out = (E*)t.out + p.agent * t.out_matrix;
   if (f == 1.0f && in == out) return;                                // (the boundary has checked that strides are the same then)
@@ -177,10 +183,10 @@ template <typename E> __device__ inline void scale(const Tensor& t, const Place&
     for (int i = 0; i < Part<E>::kVec; ++i) e[i] = (E)((float)e[i] * f);
     __builtin_memcpy(&part.v[k], e, 16);
   }
-  part.store(out, Rows(p.from, t.cols, t.out_row), p.count, t.wide);
+  part.template store<PAST>(out, Rows(p.from, t.cols, t.out_row), p.count, t.wide);
 }
 // factor NULL: every workgroup finds its agent's norm for itself, and the one with the agent's first piece of all writes it.
-template <int N> __global__ void __launch_bounds__(kThreads) k_scale(Tensors<N> a, Limits l, const float* factor, int first) {
+template <int N, bool PAST> __global__ void __launch_bounds__(kThreads) k_scale(Tensors<N> a, Limits l, const float* factor, int first) {
   __shared__ double part[4];
   const int block = gridDim.x - 1 - blockIdx.x;                      // what was read last may still be in a cache
   const Place p = place_of(a, block);
@@ -193,9 +199,9 @@ template <int N> __global__ void __launch_bounds__(kThreads) k_scale(Tensors<N> 
     f = factor_of(l, p.agent, norm);
     if (l.norms && threadIdx.x == 0 && first == 0 && block == p.agent * a.pieces) l.norms[p.agent] = (float)norm;
   }
-  if (t.dtype == POP_F32) scale<float>(t, p, f);
-  else if (t.dtype == POP_BF16) scale<__bf16>(t, p, f);
-  else scale<_Float16>(t, p, f);
+  if (t.dtype == POP_F32) scale<float, PAST>(t, p, f);
+  else if (t.dtype == POP_BF16) scale<__bf16, PAST>(t, p, f);
+  else scale<_Float16, PAST>(t, p, f);
 }
 
 int64_t all_pieces(int n, const pop_gradient* g) {
@@ -223,7 +229,7 @@ template <int N> Tensors<N> tensors_of(const ClipCall& c, int from) {
 }
 
 template <int N> void launch(const ClipCall& c, const Limits& l, float* factor, hipStream_t s) {
-  const bool few = c.max_norm && l.pieces <= kFew;
+  const bool few = c.max_norm && l.pieces <= kFew, past = (int64_t)l.pieces * c.P >= kPast;
   int first = 0;
   Tensors<N> a;
   for (int k = 0; k < c.n; k += N) {
@@ -236,7 +242,8 @@ template <int N> void launch(const ClipCall& c, const Limits& l, float* factor, 
   first = 0;
   for (int k = 0; k < c.n; k += N) {
     if (c.n > N) a = tensors_of<N>(c, k);
-    k_scale<N><<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, l, few ? nullptr : factor, first);
+    if (past) k_scale<N, true><<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, l, few ? nullptr : factor, first);
+    else k_scale<N, false><<<(unsigned)(a.pieces * c.P), kThreads, 0, s>>>(a, l, few ? nullptr : factor, first);
     first += a.pieces;
   }
 }

@@ -8,13 +8,7 @@ namespace pop {
 namespace {
 namespace linear {
 
-#ifndef POP_OCC
-#define POP_OCC 2
-#endif
-#ifndef POP_C
-#define POP_C 32
-#endif
-constexpr int kThreads = 256, kMost = POP_LINEAR_MAX_DIM;
+constexpr int kMost = POP_LINEAR_MAX_DIM;
 
 __device__ inline float log_decay_of(const float* log_decay, int at) {
   const float z = log_decay ? log_decay[at] : 0.0f;
@@ -92,9 +86,10 @@ __device__ inline void sync_lds() {
 struct Share { int chunks, per, segments, jobs; };
 enum { kMain = 0, kStates = 1 };
 
-// How a call's arrays are reached.  kWide: vectors of 16 bytes of q and k, four columns of o at a time, elements of v; kNarrow: elements, as
-// rows lie at odd places; kAny: elements by addresses of 64 bits, for steps further apart than 32 bits reach, and steps that lie
-// over each other.
+// How a call's arrays are reached.  kWide: vectors of 16 bytes from where they are aligned and a row has whole ones, four columns of o at a
+// time; kNarrow: vectors that are aligned to elements only, the last one of a row moved back to where it ends with it (rows of less than
+// a vector by elements); kAny: elements by addresses of 64 bits, for steps further apart than 32 bits reach, and steps that lie over
+// each other.
 enum { kWide = 0, kNarrow = 1, kAny = 2 };
 
 // One array of a workgroup's sequence and head, a chunk of C steps after the other (in reverse one before the other): a buffer resource
@@ -139,8 +134,10 @@ __device__ inline int channel_of(int d, int g, int i) { return 32 * (d / 2) + 8 
 // end in reverse.
 template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   static constexpr int kVec = 16 / sizeof(E), kAcross = 32 * KB / kVec, kAll = C * kAcross, kEach = (kAll + 64 * NW - 1) / (64 * NW);
-  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kIn = Parts<E>::kIn;
+  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kPairs = kVec / 2;
+  typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
+  static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
   static __device__ inline int row(int i) { return (int)(threadIdx.x + i * 64 * NW) / kAcross; }
   static __device__ inline int channel(int i) { return (int)(threadIdx.x + i * 64 * NW) % kAcross * kVec; }
   __device__ inline void load(const Steps<E, C, HOW>& a, int n, bool reverse) {
@@ -151,19 +148,41 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
       if constexpr (HOW == kWide) {
         v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, a.offset(m, channel(i)), 0, 0);
       } else {
-        E e[kVec];
+        if (HOW == kNarrow && a.width >= kVec) {                     // in front of the end of an existing row, whatever is asked for
+          const unsigned at = (unsigned)(min(m, n - 1) * (int)a.step + min(channel(i), a.width - kVec));
+          __builtin_memcpy(&v[i], a.now + at, 16);
+        } else {
+          E e[kVec];
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) e[k] = a.element(r, n, m, channel(i) + k);
-        __builtin_memcpy(&v[i], e, 16);
+          for (int k = 0; k < kVec; ++k) e[k] = a.element(r, n, m, channel(i) + k);
+          __builtin_memcpy(&v[i], e, 16);
+        }
       }
     }
   }
-  // Into LDS, part by part.  Returns whether all values are finite.
-  __device__ inline bool store(unsigned short* plane) const {
+  // What was asked for: values of the vector moved to their places, zeros behind the ends of rows and behind the last one.
+  __device__ inline void settle(const Steps<E, C, HOW>& a, int n, bool reverse) {
+    if (HOW != kNarrow || a.width < kVec) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int m = reverse ? C - 1 - row(i) : row(i), off = max(0, channel(i) - (a.width - kVec)) * (int)sizeof(E) * 8;
+      uint64_t lo = v[i][0] | (uint64_t)v[i][1] << 32, hi = v[i][2] | (uint64_t)v[i][3] << 32;
+      if (off >= 64) {
+        lo = hi;
+        hi = 0;
+      }
+      const int by = off & 63;
+      lo = lo >> by | hi << 1 << (63 - by);
+      hi >>= by;
+      const bool none = m >= n || off >= 128;
+      v[i] = u32x4{none ? 0 : (unsigned)lo, none ? 0 : (unsigned)(lo >> 32), none ? 0 : (unsigned)hi, none ? 0 : (unsigned)(hi >> 32)};
+    }
+  }
+  __device__ inline bool finite() const {
     unsigned bad = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      if (kAll % (64 * NW) != 0 && row(i) >= C) break;
+      if (!whole(i)) break;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const unsigned w = v[i][d];
@@ -171,32 +190,46 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
         else if constexpr (kIn == 1) bad |= (w & 0x7f807f80u) + 0x00800080u;
         else bad |= (w & 0x7c007c00u) + 0x04000400u;
       }
-      unsigned short* to = plane + row(i) * kStride + channel(i);
-      if constexpr (kIn == 1) {
-        *(u32x4*)to = v[i];
-      } else if constexpr (sizeof(E) == 4) {
-        unsigned lo[3], hi[3];
-        split<3>(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]), lo);
-        split<3>(__uint_as_float(v[i][2]), __uint_as_float(v[i][3]), hi);
-#pragma unroll
-        for (int n = 0; n < 3; ++n) *(u32x2*)(to + n * kPlane) = u32x2{lo[n], hi[n]};
-      } else {
-        u32x4 p[2];
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          typedef _Float16 pair __attribute__((ext_vector_type(2)));
-          const unsigned w = v[i][d];                                // (of an element in its place the cast takes the first)
-          const pair x = __builtin_bit_cast(pair, w);
-          unsigned part[2];
-          split<2>((float)x[0], (float)x[1], part);
-          p[0][d] = part[0];
-          p[1][d] = part[1];
-        }
-        *(u32x4*)to = p[0];
-        *(u32x4*)(to + kPlane) = p[1];
-      }
     }
     return (bad & (sizeof(E) == 4 ? 0x80000000u : 0x80008000u)) == 0;
+  }
+  __device__ inline void pair(int i, int d, float& a, float& b) const {
+    if constexpr (sizeof(E) == 4) {
+      a = __uint_as_float(v[i][2 * d]);
+      b = __uint_as_float(v[i][2 * d + 1]);
+    } else {
+      typedef E Two __attribute__((ext_vector_type(2)));
+      const unsigned w = v[i][d];                                    // (of an element in its place the cast takes the first)
+      const Two x = __builtin_bit_cast(Two, w);
+      a = (float)x[0];
+      b = (float)x[1];
+    }
+  }
+  static __device__ inline unsigned short* place(unsigned short* plane, int i) { return plane + row(i) * kStride + channel(i); }
+  // Into LDS, part by part.
+  __device__ inline void store(unsigned short* plane) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (!whole(i)) break;
+      if constexpr (kIn == 1) *(u32x4*)place(plane, i) = v[i];
+      else put<kIn>(plane, i, 1.0f, false);
+    }
+  }
+  // Vector i times f.
+  template <int N> __device__ inline void put(unsigned short* plane, int i, float f, bool times) const {
+    Word word[N];
+#pragma unroll
+    for (int d = 0; d < kPairs; ++d) {
+      float a, b;
+      pair(i, d, a, b);
+      unsigned part[N];
+      if (times) split<N>(a * f, b * f, part);
+      else split<N>(a, b, part);
+#pragma unroll
+      for (int n = 0; n < N; ++n) word[n][d] = part[n];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) *(Word*)(place(plane, i) + n * kPlane) = word[n];
   }
   // Rows 16 tile .. of 32 channels as an operand: a lane has channels 8 g .. 8 g + 7.
   static __device__ inline Operand<kIn> rows(const unsigned short* plane, int tile, int kb, int lane) {
@@ -206,13 +239,13 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     for (int n = 0; n < kIn; ++n) o.part[n] = *(const u32x4*)(from + n * kPlane);
     return o;
   }
-  // The channels of half `d % 2` of block d / 2 (channel_of) of 32 rows as an operand: four rows of four times four channels, turned over by
-  // the read.
-  static __device__ inline Operand<kIn> channels(unsigned short* plane, int block, int d, int lane) {
-    Operand<kIn> o;
-    unsigned short* from = plane + (32 * block + 4 * (lane >> 4) + (lane & 15) / 4) * kStride + channel_of(d, lane & 3, 0);
+  // Sixteen channels of 32 rows as an operand, four rows of four times four channels turned over by the read: those of half `d % 2` of block
+  // d / 2 (channel_of), and 16 w .. 16 w + 15.
+  template <int N> static __device__ inline Operand<N> turned(unsigned short* plane, int first, int lane) {
+    Operand<N> o;
+    unsigned short* from = plane + (4 * (lane >> 4) + (lane & 15) / 4) * kStride + first;
 #pragma unroll
-    for (int n = 0; n < kIn; ++n) {
+    for (int n = 0; n < N; ++n) {
       const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kPlane));
       const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kPlane + 16 * kStride));
       const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
@@ -220,24 +253,32 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     }
     return o;
   }
+  static __device__ inline Operand<kOf> channels(unsigned short* plane, int d, int lane) { return turned<kOf>(plane, channel_of(d, lane & 3, 0), lane); }
+  static __device__ inline Operand<kIn> columns(unsigned short* plane, int w, int lane) { return turned<kIn>(plane, 16 * w + 4 * (lane & 3), lane); }
 };
 
 __device__ inline float power(float log2_decay, int n) { return __builtin_amdgcn_exp2f((float)n * log2_decay); }
 __device__ inline bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
 
-// A wavefront has 16 VT of the state's columns, the workgroup those of NW wavefronts.
-template <typename E, int KB, int NW, int VT, int C, int HOW>
-__global__ void __launch_bounds__(64 * NW, POP_OCC) k_chunks(LinearArgs a, Share share, float* ws, int mode) {
+template <typename E, int KB> constexpr int waves_per_simd() { return sizeof(E) == 2 && KB <= 2 ? 3 : 2; }
+
+// A wavefront has 16 of the state's columns, the workgroup those of NW wavefronts.
+template <typename E, int KB, int NW, int C, int HOW>
+__global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(LinearArgs a, Share share, float* ws, int mode, int jobs) {
   typedef Tile<E, KB, NW, C, HOW> T;
+  typedef Tile<E, NW / 2, NW, C, HOW> TV;
   typedef Steps<E, C, HOW> Array;
-  constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kTiles = C / 16, kBlocks = C / 32;
-  static_assert(C == 32, "starts of episodes are the bits of a word");
-  __shared__ __attribute__((aligned(16))) unsigned short lds[2 * kIn * T::kPlane];
-  __shared__ int bad_keys[2];
-  unsigned short *const keys = lds, *const queries = lds + kIn * T::kPlane;
-  const LinearRole& role = a.role[blockIdx.z];
-  const int col = blockIdx.x, seg = blockIdx.y, h = col % a.H, row = col / a.H, b = row % a.B, p = row / a.B;
+  constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf;
+  static_assert(C == 32, "two tiles of rows; starts of episodes are the bits of a word");
+  __shared__ __attribute__((aligned(16))) unsigned short keys[kIn * T::kPlane], queries[kIn * T::kPlane], faded[kOf * T::kPlane], values[kIn * TV::kPlane];
+  __shared__ u32x2 shared_weights[3][kOf][64];
+  __shared__ int bad[2];
+  // the roles of a column one after the other on one XCD: they read the same arrays
+  const int job = blockIdx.x / 8 % jobs, unit = blockIdx.x / (8 * jobs) * 8 + blockIdx.x % 8, cols = a.P * a.B * a.H;
+  if (unit >= cols * share.segments) return;
+  const LinearRole& role = a.role[job];
+  const int seg = unit / cols, col = unit - seg * cols, h = col % a.H, row = col / a.H, b = row % a.B, p = row / a.B;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, at = lane & 15, K = role.K, V = role.V;
   const bool reverse = role.reverse, states = mode == kStates;
   const int len = a.lengths ? min(max(a.lengths[row], 0), a.T) : a.T;
@@ -248,67 +289,55 @@ __global__ void __launch_bounds__(64 * NW, POP_OCC) k_chunks(LinearArgs a, Share
   const int start = from * C, end = min(until * C, a.T), n_chunks = max(0, (min(end, len) - start + C - 1) / C);
   const int first_t = start + (reverse ? max(n_chunks - 1, 0) * C : 0);
   Array q(role.q, p, b, h, K, first_t, reverse), k(role.k, p, b, h, K, first_t, reverse), v(role.v, p, b, h, V, first_t, reverse), o(role.o, p, b, h, V, first_t, reverse);
-  const int first_column = 16 * VT * wave;                           // this lane's columns: first_column + 16 c + at
-  const bool idle = first_column >= V;                               // a wave with no columns loads with the others
+  const int column = 16 * wave + at;
+  const bool idle = 16 * wave >= V;                                  // a wave with no columns loads with the others
 
-  // the state: S[c][d][i] is channel channel_of(d, g, i) of column c
-  f32x4 S[VT][2 * KB];
+  // the state: S[d][i] is channel channel_of(d, g, i) of this lane's column
+  f32x4 S[2 * KB];
   bool tainted = false;
   {
     const float* first = states ? nullptr : share.segments > 1 ? ws : role.first;
     int64_t base = (int64_t)col * K * V;
     int along_k = role.first_k, along_v = role.first_v;
     if (share.segments > 1) {
-      const int job = blockIdx.z == 2 ? 1 : blockIdx.z;              // role 2 takes the states of role 1, transposed
-      base += ((int64_t)job * share.segments + seg) * gridDim.x * K * V;
-      along_k = blockIdx.z == 2 ? 1 : V;
-      along_v = blockIdx.z == 2 ? K : 1;
+      // role 2 takes the states of role 1, transposed
+      base += ((int64_t)min(job, 1) * share.segments + seg) * cols * K * V;
+      along_k = job == 2 ? 1 : V;
+      along_v = job == 2 ? K : 1;
     }
 #pragma unroll
-    for (int c = 0; c < VT; ++c)
+    for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
-      for (int d = 0; d < 2 * KB; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row_k = channel_of(d, g, i), column = first_column + 16 * c + at;
-          S[c][d][i] = first && row_k < K && column < V ? first[base + row_k * along_k + column * along_v] : 0.0f;
-          tainted |= not_finite(S[c][d][i]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const int row_k = channel_of(d, g, i);
+        S[d][i] = first && row_k < K && column < V ? first[base + row_k * along_k + column * along_v] : 0.0f;
+        tainted |= not_finite(S[d][i]);
+      }
     tainted = any_lane(tainted);
   }
 
-  // Weights of pairs, row `at` of a tile and row 4 g + j of another: the same tile, one in front; further ones by a power for the tile.
-  // Weights of the state on its way in and out.
+  // Weights of pairs, row `at` of a tile and row 4 g + j of the same one, or of the one in front.  Weights of the state on its way in, and of
+  // this thread's rows of keys on their way out.
   const float both = role.read * role.write, whole = power(l2, C);
-  float here[4], there[4], tiles[kTiles], into[kTiles], outof[kTiles][4];
+  float here[4], there[4], into[2], outof[T::kEach];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     here[j] = both * power(l2, max(at - 4 * g - j, 0));
     there[j] = both * power(l2, 16 + at - 4 * g - j);
   }
 #pragma unroll
-  for (int n = 0; n < kTiles; ++n) {
-    tiles[n] = power(l2, 16 * n);
-    into[n] = role.read * power(l2, 16 * n + at + before);
+  for (int n = 0; n < 2; ++n) into[n] = role.read * power(l2, 16 * n + at + before);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) outof[n][j] = role.write * power(l2, C - 1 - (16 * n + 4 * g + j) + behind);
-  }
+  for (int i = 0; i < T::kEach; ++i) outof[i] = role.write * power(l2, max(C - 1 - T::row(i), 0) + behind);
 
   T next_k, next_q;
-  E next_v[VT][C / 4];
+  TV next_v;
   uint8_t next_cut = 0;
   const auto load = [&](int n) {
     const int t = start + (reverse ? n_chunks - 1 - n : n) * C, count = min(C, len - t);
     next_k.load(k, count, reverse);
     if (!states) next_q.load(q, count, reverse);
-    const auto r = v.chunk(count);
-#pragma unroll
-    for (int c = 0; c < VT; ++c)
-#pragma unroll
-      for (int j = 0; j < C / 4; ++j) {
-        const int s = 16 * (j / 4) + 4 * g + j % 4, m = reverse ? C - 1 - s : s, column = first_column + 16 * c + at;
-        next_v[c][j] = v.element(r, count, m, column);
-      }
+    next_v.load(v, count, reverse);
     k.now += k.hop;
     q.now += q.hop;
     v.now += v.hop;
@@ -318,277 +347,290 @@ __global__ void __launch_bounds__(64 * NW, POP_OCC) k_chunks(LinearArgs a, Share
     }
   };
   if (n_chunks > 0) load(0);
-  if (threadIdx.x == 0) bad_keys[0] = 0;
+  if (threadIdx.x == 0) bad[0] = 0;
+  if (n_chunks > 0) sync_lds();
   bool any_cut = false;
 
   for (int n = 0; n < n_chunks; ++n) {
     const int t = start + (reverse ? n_chunks - 1 - n : n) * C, count = min(C, len - t);
     if (n > 0) o.now += o.hop;
-    sync_lds();                                                      // the chunk before has been read
-    if (!next_k.store(keys)) bad_keys[n & 1] = 1;
-    if (!states) next_q.store(queries);
     const unsigned cuts = (unsigned)__builtin_amdgcn_ballot_w64(next_cut != 0);
-    f32x4 value[VT][kTiles];
-    float zero = 0.0f;                                               // but where a value is not finite
+    any_cut |= cuts != 0;
+    const bool regular = cuts == 0 && count == C;
+    const auto starts = [&](int r) { return __popc(cuts & ((2u << here_only(r)) - 1)); };   // episodes that start at rows 0 .. r
+    const int all_starts = __popc(cuts);
+    next_k.settle(k, count, reverse);
+    next_v.settle(v, count, reverse);
+    next_v.store(values);
+    bool fine = next_k.finite() & next_v.finite();
+    if (!states) {
+      next_q.settle(q, count, reverse);
+      next_k.store(keys);
+      next_q.store(queries);
+      fine &= next_q.finite();
+    }
+    if (!fine) bad[n & 1] = 1;
 #pragma unroll
-    for (int c = 0; c < VT; ++c)
-#pragma unroll
-      for (int j = 0; j < C / 4; ++j) {
-        value[c][j / 4][j % 4] = (float)next_v[c][j];
-        zero = fmaf((float)next_v[c][j], 0.0f, zero);
+    for (int i = 0; i < T::kEach; ++i) {
+      if (!T::whole(i)) break;
+      float f = outof[i];
+      if (!regular) {
+        const int r = here_only(T::row(i));
+        if (!reverse) f = role.write * power(l2, max(count - 1 - r, 0));
+        f = starts(r) == all_starts ? f : 0.0f;
       }
+      next_k.template put<kOf>(faded, i, f, true);
+    }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
-    const bool slow = __builtin_amdgcn_readfirstlane(bad_keys[n & 1]) != 0 || any_lane(zero != 0.0f) || tainted;
-    if (threadIdx.x == 0) bad_keys[(n + 1) & 1] = 0;
-    any_cut |= cuts != 0;
-    if (idle) continue;
+    const bool slow = __builtin_amdgcn_readfirstlane(bad[n & 1]) != 0 || tainted;
+    if (threadIdx.x == 0) bad[(n + 1) & 1] = 0;
 
-    if (__builtin_expect(slow, 0)) {
+    if (!states) {
+      // the weights of pairs of rows, for all wavefronts: tiles 0 and 1 with themselves, 1 with 0
+      for (int w = NW - 1 - wave; w < 3; w += NW) {
+        const int queried = w > 0, other = w == 1;
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int d = 0; d < KB; ++d) x = product(T::rows(keys, other, d, lane), T::rows(queries, queried, d, lane), x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (w < 2) x[j] = 4 * g + j <= at ? x[j] * here[j] : 0.0f;
+          else x[j] *= there[j];
+        }
+        if (!regular) {
+          const int mine = starts(16 * queried + at);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = starts(16 * other + 4 * g + j) == mine ? x[j] : 0.0f;
+        }
+        unsigned lo[kOf], hi[kOf];
+        split<kOf>(x[0], x[1], lo);
+        split<kOf>(x[2], x[3], hi);
+#pragma unroll
+        for (int n = 0; n < kOf; ++n) shared_weights[w][n][lane] = u32x2{lo[n], hi[n]};
+      }
+    }
+
+    f32x4 out[2];                                                    // rows: columns 4 g + i of the wave's; column: row `at` of the tile
+    Operand<kIn> value;
+    if (idle) {
+    } else if (__builtin_expect(slow, 0)) {
       // something here is not finite, and a product with a weight of zero would carry it where it does not belong: step by step
       tainted = false;
       const E *qs = linear::at<E>(role.q, p, b, h), *ks = linear::at<E>(role.k, p, b, h), *vs = linear::at<E>(role.v, p, b, h);
       E* os = (E*)linear::at<E>(role.o, p, b, h);
+      const int g = here_only(lane >> 4), column = 16 * wave + here_only(lane & 15);
 #pragma unroll 1
       for (int r = reverse ? C - count : 0; r < (reverse ? C : count); ++r) {
         const int64_t s = t + (reverse ? C - 1 - r : r);
         const bool cut = cuts >> r & 1;
-        const int g = here_only(lane >> 4), at = here_only(lane & 15);
-#pragma unroll
-        for (int c = 0; c < VT; ++c) {
-          const int column = first_column + 16 * c + at;
-          const float vr = column < V ? (float)vs[s * role.v.step + column] * role.write : 0.0f;
-          float sum = 0.0f;
-#pragma unroll
-          for (int d = 0; d < 2 * KB; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int kr = channel_of(d, g, i);
-              if (kr < K) {
-                const float x = fmaf((float)ks[s * role.k.step + kr], vr, cut ? 0.0f : reverse ? S[c][d][i] : lambda * S[c][d][i]);
-                if (!states) sum = fmaf((float)qs[s * role.q.step + kr], x, sum);
-                S[c][d][i] = reverse ? lambda * x : x;
-              }
-            }
-          sum += __shfl_xor(sum, 16);
-          sum += __shfl_xor(sum, 32);
-          if (!states && g == 0 && column < V) os[s * role.o.step + column] = (E)(sum * role.read);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < VT; ++c)
+        const float vr = column < V ? (float)vs[s * role.v.step + column] * role.write : 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tainted |= not_finite(S[c][d][i]);
+          for (int i = 0; i < 4; ++i) {
+            const int kr = channel_of(d, g, i);
+            if (kr < K) {
+              const float x = fmaf((float)ks[s * role.k.step + kr], vr, cut ? 0.0f : reverse ? S[d][i] : lambda * S[d][i]);
+              if (!states) sum = fmaf((float)qs[s * role.q.step + kr], x, sum);
+              S[d][i] = reverse ? lambda * x : x;
+            }
+          }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (!states && g == 0 && column < V) os[s * role.o.step + column] = (E)(sum * role.read);
+      }
+#pragma unroll
+      for (int d = 0; d < 2 * KB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tainted |= not_finite(S[d][i]);
       tainted = any_lane(tainted);
-      continue;
+    } else {
+      value = TV::columns(values, wave, lane);
+      if (!states) {
+        Operand<kOf> memory[KB];
+#pragma unroll
+        for (int d = 0; d < KB; ++d) memory[d] = operand<kOf>(S[2 * d], S[2 * d + 1]);
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) {
+          out[tile] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int d = 0; d < KB; ++d) out[tile] = product(memory[d], T::rows(queries, tile, d, lane), out[tile]);
+          float f = into[tile];
+          if (!regular && reverse) f = role.read * power(l2, max(16 * tile + here_only(at) - (C - count), 0));
+          out[tile] *= f;
+          if (all_starts != 0) {
+            const bool own = starts(16 * tile + at) != 0;            // nothing of the state
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[tile][e] = own ? 0.0f : out[tile][e];
+          }
+        }
+      }
+      float keep = whole;
+      if (!regular) keep = power(l2, count);
+      if (all_starts != 0) {
+#pragma unroll
+        for (int d = 0; d < 2 * KB; ++d) S[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+#pragma unroll
+      for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::channels(faded, d, lane), value, S[d] * keep);
     }
+    sync_lds();                                                      // all of the chunk has been read but the weights, which are written
 
-    const bool regular = cuts == 0 && count == C;
-    const auto starts = [&](int r) { return __popc(cuts & ((2u << here_only(r)) - 1)); };   // episodes that start at rows 0 .. r
-    const int all_starts = __popc(cuts);
-
-    if (!states) {
-      Operand<kIn> values[VT][kBlocks];
-      Operand<kOf> memory[VT][KB];
+    if (states || idle || slow) continue;
+    const auto r = o.chunk(count);
 #pragma unroll
-      for (int c = 0; c < VT; ++c) {
+    for (int tile = 0; tile < 2; ++tile) {
+      Operand<kOf> weights;
 #pragma unroll
-        for (int s = 0; s < kBlocks; ++s) values[c][s] = operand<kIn>(value[c][2 * s], value[c][2 * s + 1]);
-#pragma unroll
-        for (int d = 0; d < KB; ++d) memory[c][d] = operand<kOf>(S[c][2 * d], S[c][2 * d + 1]);
+      for (int n = 0; n < kOf; ++n) {
+        const u32x2 lo = shared_weights[tile == 0 ? 0 : 2][n][lane], hi = shared_weights[1][n][lane];
+        weights.part[n] = tile == 0 ? u32x4{lo[0], lo[1], 0, 0} : u32x4{lo[0], lo[1], hi[0], hi[1]};
       }
-      const auto r = o.chunk(count);
+      const f32x4 y = product(value, weights, out[tile]);
+      typedef E Four __attribute__((ext_vector_type(4)));
+      const Four x = {(E)y[0], (E)y[1], (E)y[2], (E)y[3]};
+      const int i = 16 * tile + at, m = reverse ? C - 1 - i : i, column = 16 * wave + 4 * g;
+      if constexpr (HOW == kWide) {
+        if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, o.offset(m, column), 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, x), r, o.offset(m, column), 0, 0);
+      } else {
+        if (HOW == kNarrow && column + 4 <= V) {
+          if (m < count) __builtin_memcpy(o.now + (unsigned)(m * (int)o.step + column), &x, sizeof(Four));
+        } else {
 #pragma unroll
-      for (int tile = 0; tile < kTiles; ++tile) {
-        Operand<kIn> query[KB];
-        f32x4 out[VT];                                               // rows: columns 4 g + i of 16; column: row `at` of the tile
-#pragma unroll
-        for (int c = 0; c < VT; ++c) out[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int d = 0; d < KB; ++d) {
-          query[d] = T::rows(queries, tile, d, lane);
-#pragma unroll
-          for (int c = 0; c < VT; ++c) out[c] = product(memory[c][d], query[d], out[c]);
-        }
-        const int i = 16 * tile + at;
-        int mine = 0;
-        float f = into[tile];
-        if (!regular) {
-          mine = starts(i);
-          if (reverse) f = role.read * power(l2, max(here_only(i) - (C - count), 0));
-        }
-#pragma unroll
-        for (int c = 0; c < VT; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[c][e] = mine == 0 ? out[c][e] * f : 0.0f;
-#pragma unroll
-        for (int block = 0; block <= tile / 2; ++block) {
-          f32x4 weight[2];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int other = 2 * block + half;
-            f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (other <= tile) {
-#pragma unroll
-              for (int d = 0; d < KB; ++d) w = product(T::rows(keys, other, d, lane), query[d], w);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if (other == tile) w[j] = 4 * g + j <= at ? w[j] * here[j] : 0.0f;
-                else w[j] *= other + 1 == tile ? there[j] : there[j] * tiles[tile - other - 1];
-              }
-              if (!regular)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = starts(16 * other + 4 * g + j) == mine ? w[j] : 0.0f;
-            }
-            weight[half] = w;
-          }
-          const Operand<kOf> weights = operand<kOf>(weight[0], weight[1]);
-#pragma unroll
-          for (int c = 0; c < VT; ++c) out[c] = product(values[c][block], weights, out[c]);
-        }
-        const int m = reverse ? C - 1 - i : i;
-#pragma unroll
-        for (int c = 0; c < VT; ++c) {
-          typedef E Four __attribute__((ext_vector_type(4)));
-          const Four x = {(E)out[c][0], (E)out[c][1], (E)out[c][2], (E)out[c][3]};
-          const int column = first_column + 16 * c + 4 * g;
-          if constexpr (HOW == kWide) {
-            if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, o.offset(m, column), 0, 0);
-            else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, x), r, o.offset(m, column), 0, 0);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const E y = x[e];
-              o.put(r, count, m, column + e, y);
-            }
+          for (int e = 0; e < 4; ++e) {
+            const E y = x[e];
+            o.put(r, count, m, column + e, y);
           }
         }
-      }
-    }
-
-    float keep = whole;
-    if (!regular) keep = power(l2, count);
-#pragma unroll
-    for (int c = 0; c < VT; ++c) {
-      Operand<kOf> faded[kBlocks];
-#pragma unroll
-      for (int s = 0; s < kBlocks; ++s) {
-        f32x4 x[2];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int r = 32 * s + 16 * (j / 4) + 4 * g + j % 4;
-          float f = outof[2 * s + j / 4][j % 4];
-          if (!regular) {
-            if (!reverse) f = role.write * power(l2, max(count - 1 - here_only(r), 0));
-            f = starts(r) == all_starts ? f : 0.0f;
-          }
-          x[j / 4][j % 4] = value[c][2 * s + j / 4][j % 4] * f;
-        }
-        faded[s] = operand<kOf>(x[0], x[1]);
-      }
-#pragma unroll
-      for (int d = 0; d < 2 * KB; ++d) {
-        f32x4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = all_starts == 0 ? S[c][d][i] * keep : 0.0f;
-#pragma unroll
-        for (int s = 0; s < kBlocks; ++s) x = product(T::channels(keys, s, d, lane), faded[s], x);
-        S[c][d] = x;
       }
     }
   }
 
-#pragma unroll
-  for (int c = 0; c < VT; ++c) {
-    const int column = first_column + 16 * c + at;
-    if (!states && column < V)
-      for (int t = max(start, len) + g; t < end; t += 4) ((E*)linear::at<E>(role.o, p, b, h))[t * role.o.step + column] = (E)0.0f;
-  }
+  if (!states && column < V)
+    for (int t = max(start, len) + g; t < end; t += 4) ((E*)linear::at<E>(role.o, p, b, h))[t * role.o.step + column] = (E)0.0f;
   const bool last = seg == share.segments - 1;
-  float* to = states ? ws + (((int64_t)blockIdx.z * share.segments + seg) * gridDim.x + col) * K * V : last && role.last ? role.last + (int64_t)col * K * V : nullptr;
+  float* to = states ? ws + (((int64_t)job * share.segments + seg) * cols + col) * K * V : last && role.last ? role.last + (int64_t)col * K * V : nullptr;
   if (!to) return;
   const bool cut = !states && reverse && len > 0 && reset && reset[0];
 #pragma unroll
-  for (int c = 0; c < VT; ++c)
+  for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
-    for (int d = 0; d < 2 * KB; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row_k = channel_of(d, g, i), column = first_column + 16 * c + at;
-        if (row_k < K && column < V) to[row_k * V + column] = cut ? 0.0f : S[c][d][i];
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int row_k = channel_of(d, g, i);
+      if (row_k < K && column < V) to[row_k * V + column] = cut ? 0.0f : S[d][i];
+    }
   if (states && threadIdx.x == 0) {
-    float* factor = ws + (int64_t)share.jobs * share.segments * gridDim.x * K * V;
-    factor[((int64_t)blockIdx.z * share.segments + seg) * gridDim.x + col] = any_cut ? -1.0f : power(l2, max(0, min(end, len) - start));
+    float* factor = ws + (int64_t)share.jobs * share.segments * cols * K * V;
+    factor[((int64_t)job * share.segments + seg) * cols + col] = any_cut ? -1.0f : power(l2, max(0, min(end, len) - start));
   }
 }
 
 // The states in front of the segments, in the places of what the segments add to them.  A negative factor: nothing of the state in front
 // is left.
-__global__ void __launch_bounds__(kThreads) k_scan(LinearArgs a, Share share, float* ws, int cols) {
+constexpr int kScan = 64;
+template <int AHEAD> __global__ void __launch_bounds__(kScan) k_scan(LinearArgs a, Share share, float* ws, int cols) {
   const LinearRole& role = a.role[blockIdx.y];
-  const int64_t size = (int64_t)role.K * role.V, n = cols * size, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int size = role.K * role.V, n = cols * size, i = blockIdx.x * kScan + threadIdx.x;    // few columns: n is below 2^24
   if (i >= n) return;
-  const int col = (int)(i / size), e = (int)(i % size);
+  const int col = i / size, e = i - col * size;
   float* at = ws + (int64_t)blockIdx.y * share.segments * n + i;
   const float* factor = ws + (int64_t)share.jobs * share.segments * n + (int64_t)blockIdx.y * share.segments * cols + col;
-  float s = role.first ? role.first[col * size + e / role.V * role.first_k + e % role.V * role.first_v] : 0.0f;
-  float add = at[0], f = factor[0];
-  for (int k = 0; k < share.segments; ++k) {
-    const float add_now = add, f_now = f;
-    if (k + 1 < share.segments) {
-      add = at[(k + 1) * n];
-      f = factor[(int64_t)(k + 1) * cols];
+  float s = role.first ? role.first[(int64_t)col * size + e / role.V * role.first_k + e % role.V * role.first_v] : 0.0f;
+  for (int k = 0; k < share.segments; k += AHEAD) {
+    float add[AHEAD], f[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int from = min(k + u, share.segments - 1);
+      add[u] = at[(int64_t)from * n];
+      f[u] = factor[from * cols];
     }
-    at[k * n] = s;
-    s = f_now < 0.0f ? add_now : fmaf(f_now, s, add_now);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k + u >= share.segments) break;
+      at[(int64_t)(k + u) * n] = s;
+      s = f[u] < 0.0f ? add[u] : fmaf(f[u], s, add[u]);
+    }
   }
 }
 
-template <typename E> __global__ void __launch_bounds__(kThreads) k_step(LinearStep a) {
-  __shared__ float sq[kMost], sk[kMost], part[kThreads];
+// A workgroup of NW wavefronts per row and head; a thread has four columns of every so many'th row of the state.
+template <typename E, int NW> __global__ void __launch_bounds__(64 * NW) k_step(LinearStep a) {
+  constexpr int kStep = 64 * NW, kRows = 4;
+  __shared__ float sq[kMost], sk[kMost], part[NW][kMost];
   const int h = blockIdx.x % a.H, row = blockIdx.x / a.H, b = row % a.B, p = row / a.B;
   const int slot = a.slots ? a.slots[row] : b;
   E* o = (E*)a.o.data + p * a.o.agent + b * a.o.row + h * a.o.head;
   if (slot < 0 || slot >= a.n_slots) {
-    for (int i = threadIdx.x; i < a.V; i += kThreads) o[i] = (E)0.0f;
+    for (int i = threadIdx.x; i < a.V; i += kStep) o[i] = (E)0.0f;
     return;
   }
-  for (int i = threadIdx.x; i < a.K; i += kThreads) {
+  for (int i = threadIdx.x; i < a.K; i += kStep) {
     sq[i] = (float)at<E>(a.q, p, b, h)[i];
     sk[i] = (float)at<E>(a.k, p, b, h)[i];
   }
   const bool cut = a.reset.data && ((const uint8_t*)a.reset.data)[p * a.reset.agent + b * a.reset.row];
   const float lambda = expf(log_decay_of(a.log_decay, p * a.H + h));
-  int width = 1;
-  while (width < a.V) width *= 2;
-  const int groups = kThreads / width, j = threadIdx.x % width, g = threadIdx.x / width;
-  float* S = a.state + (((int64_t)p * a.n_slots + slot) * a.H + h) * a.K * a.V;
-  __syncthreads();
-  float sum = 0.0f;
-  if (j < a.V) {
-    const float v = (float)at<E>(a.v, p, b, h)[j];
-    for (int k = g; k < a.K; k += groups) {
-      const float s = fmaf(sk[k], v, cut ? 0.0f : lambda * S[k * a.V + j]);
-      S[k * a.V + j] = s;
-      sum = fmaf(sq[k], s, sum);
+  const int quads = (a.V + 3) / 4, shift = quads > 1 ? 32 - __clz(quads - 1) : 0, width = 1 << shift, hop = kStep >> shift;
+  const int column = 4 * (threadIdx.x & (width - 1)), n = min(4, a.V - column);      // n <= 0: none
+  float* S = a.state + (((int64_t)p * a.n_slots + slot) * a.H + h) * a.K * a.V + column;
+  float v[4], sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] = c < n ? (float)at<E>(a.v, p, b, h)[column + c] : 0.0f;
+  for (int first = threadIdx.x >> shift; first - (int)(threadIdx.x >> shift) < a.K; first += kRows * hop) {
+    f32x4 s[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int k = first + r * hop;
+      s[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (!cut && k < a.K) {
+        if (n == 4) __builtin_memcpy(&s[r], S + k * a.V, 16);
+        else
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+            if (c < n) s[r][c] = S[k * a.V + c];
+      }
+    }
+    if (first == (int)(threadIdx.x >> shift)) __syncthreads();       // (for all threads in the first round)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const int k = first + r * hop;
+      if (k < a.K) {
+        const float key = sk[k], query = sq[k];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s[r][c] = fmaf(key, v[c], lambda * s[r][c]);
+          sum[c] = fmaf(query, s[r][c], sum[c]);
+        }
+        if (n == 4) __builtin_memcpy(S + k * a.V, &s[r], 16);
+        else
+#pragma unroll
+          for (int c = 0; c < 3; ++c)
+            if (c < n) S[k * a.V + c] = s[r][c];
+      }
     }
   }
-  part[threadIdx.x] = sum;
+  for (int d = width; d < 64; d *= 2)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sum[c] += __shfl_xor(sum[c], d);
+  if ((threadIdx.x & 63) < width)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) part[threadIdx.x >> 6][column + c] = sum[c];
   __syncthreads();
-  if (g == 0 && j < a.V) {
-    for (int i = 1; i < groups; ++i) sum += part[i * width + j];
-    o[j] = (E)(sum * a.scale);
+  for (int i = threadIdx.x; i < a.V; i += kStep) {
+    float all = part[0][i];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) all += part[w][i];
+    o[i] = (E)(all * a.scale);
   }
 }
 
 // Sequences are cut into segments where there are too few of them: the segments' own states first, then those in front of them.
-constexpr int kChunk = POP_C, kWorkgroups = 1024, kLeast = 4, kMostSegments = 4096;
-template <typename E> constexpr int chunk_of(int K) { return kChunk; }
-Share share_of(int64_t cols, int64_t T, int chunk, bool backward) {
-  const int64_t chunks = (T + chunk - 1) / chunk, roles = backward ? 3 : 1;
+constexpr int kChunk = 32, kWorkgroups = 1024, kLeast = 4, kMostSegments = 4096;
+Share share_of(int64_t cols, int64_t T, bool backward) {
+  const int64_t chunks = (T + kChunk - 1) / kChunk, roles = backward ? 3 : 1;
   int64_t want = kWorkgroups / (cols * roles);
   if (want > kMostSegments) want = kMostSegments;
   if (want > chunks / kLeast) want = chunks / kLeast;
@@ -597,27 +639,19 @@ Share share_of(int64_t cols, int64_t T, int chunk, bool backward) {
   return {(int)chunks, (int)per, (int)((chunks + per - 1) / per), backward ? 2 : 1};
 }
 
-#ifndef POP_VT
-#define POP_VT 1
-#endif
-template <typename E, int KB, int NW, int HOW> void chunks(const LinearArgs& a, const Share& share, float* ws, int mode, dim3 grid, hipStream_t s) {
-  constexpr int VT = NW >= 2 * POP_VT ? POP_VT : 1;
-  k_chunks<E, KB, NW / VT, VT, kChunk, HOW><<<grid, 64 * NW / VT, 0, s>>>(a, share, ws, mode);
+typedef void (*Kernel)(LinearArgs, Share, float*, int, int);
+template <typename E, int KB, int HOW> Kernel kernel_of(int V) {
+  return V > 64 ? k_chunks<E, KB, 8, kChunk, HOW> : V > 32 ? k_chunks<E, KB, 4, kChunk, HOW> : k_chunks<E, KB, 2, kChunk, HOW>;
 }
-template <typename E, int KB, int HOW> void launch(const LinearArgs& a, const Share& share, float* ws, int mode, dim3 grid, int V, hipStream_t s) {
-  if (V > 64) chunks<E, KB, 8, HOW>(a, share, ws, mode, grid, s);
-  else if (V > 32) chunks<E, KB, 4, HOW>(a, share, ws, mode, grid, s);
-  else chunks<E, KB, 2, HOW>(a, share, ws, mode, grid, s);
+template <typename E, int HOW> Kernel kernel_of(int K, int V) {
+  return K <= 32 ? kernel_of<E, 1, HOW>(V) : K <= 64 ? kernel_of<E, 2, HOW>(V) : kernel_of<E, 4, HOW>(V);
 }
-template <typename E, int HOW> void launch(const LinearArgs& a, const Share& share, float* ws, int mode, dim3 grid, int K, int V, hipStream_t s) {
-  if (K <= 32) launch<E, 1, HOW>(a, share, ws, mode, grid, V, s);
-  else if (K <= 64) launch<E, 2, HOW>(a, share, ws, mode, grid, V, s);
-  else launch<E, 4, HOW>(a, share, ws, mode, grid, V, s);
-}
-template <typename E> void launch(int how, const LinearArgs& a, const Share& share, float* ws, int mode, dim3 grid, int K, int V, hipStream_t s) {
-  if (how == kWide) launch<E, kWide>(a, share, ws, mode, grid, K, V, s);
-  else if (how == kNarrow) launch<E, kNarrow>(a, share, ws, mode, grid, K, V, s);
-  else chunks<E, POP_LINEAR_MAX_DIM / 32, POP_LINEAR_MAX_DIM / 16, kAny>(a, share, ws, mode, grid, s);
+template <typename E> void launch(int how, const LinearArgs& a, const Share& share, float* ws, int mode, int jobs, int K, int V, hipStream_t s) {
+  constexpr int kAll = POP_LINEAR_MAX_DIM;
+  const Kernel k = how == kWide ? kernel_of<E, kWide>(K, V) : how == kNarrow ? kernel_of<E, kNarrow>(K, V) : k_chunks<E, kAll / 32, kAll / 16, kChunk, kAny>;
+  const int waves = how == kAny || V > 64 ? 8 : V > 32 ? 4 : 2;
+  const unsigned cols = (unsigned)(a.P * a.B * a.H);
+  k<<<(cols * share.segments + 7) / 8 * 8 * jobs, 64 * waves, 0, s>>>(a, share, ws, mode, jobs);
 }
 template <typename E> int how_of(const LinearArgs& a) {
   int how = kWide;
@@ -628,36 +662,39 @@ template <typename E> int how_of(const LinearArgs& a) {
     };
     const auto near = [](const pop_heads& s, int width) { return s.step >= width && s.step < (int64_t)((1u << 30) / sizeof(E)) / kChunk; };
     if (!near(r.q, r.K) || !near(r.k, r.K) || !near(r.v, r.V) || !near(r.o, r.V)) return kAny;
-    if (!aligned(r.q, r.K, 16 / sizeof(E)) || !aligned(r.k, r.K, 16 / sizeof(E)) || !aligned(r.o, r.V, 4)) how = kNarrow;
+    constexpr int n = 16 / sizeof(E);
+    if (!aligned(r.q, r.K, n) || !aligned(r.k, r.K, n) || !aligned(r.v, r.V, n) || !aligned(r.o, r.V, 4)) how = kNarrow;
   }
   return how;
 }
 template <typename E> hipError_t run(const LinearArgs& a, float* ws, hipStream_t s) {
-  const int64_t cols = (int64_t)a.P * a.B * a.H;
-  // roles of one shape go together
-  const int K = a.role[0].K > a.role[0].V ? a.role[0].K : a.role[0].V;
-  const Share share = share_of(cols, a.T, chunk_of<E>(a.roles > 1 ? K : a.role[0].K), a.roles > 1);
-  const int kk = a.roles > 1 ? K : a.role[0].K, vv = a.roles > 1 ? K : a.role[0].V;
+  const int cols = a.P * a.B * a.H;
+  const Share share = share_of(cols, a.T, a.roles > 1);
+  // roles go together, in a kernel that is wide enough for all
+  const int most = a.role[0].K > a.role[0].V ? a.role[0].K : a.role[0].V, K = a.roles > 1 ? most : a.role[0].K, V = a.roles > 1 ? most : a.role[0].V;
   const int how = how_of<E>(a);
   if (share.segments > 1) {
-    launch<E>(how, a, share, ws, kStates, dim3((unsigned)cols, share.segments, share.jobs), kk, vv, s);
-    k_scan<<<dim3((unsigned)((cols * a.role[0].K * a.role[0].V + kThreads - 1) / kThreads), share.jobs), kThreads, 0, s>>>(a, share, ws, (int)cols);
+    launch<E>(how, a, share, ws, kStates, share.jobs, K, V, s);
+    const dim3 grid((cols * a.role[0].K * a.role[0].V + kScan - 1) / kScan, share.jobs);
+    if (share.segments <= 8) k_scan<4><<<grid, kScan, 0, s>>>(a, share, ws, cols);
+    else k_scan<16><<<grid, kScan, 0, s>>>(a, share, ws, cols);
   }
-  launch<E>(how, a, share, ws, kMain, dim3((unsigned)cols, share.segments, a.roles), kk, vv, s);
+  launch<E>(how, a, share, ws, kMain, a.roles, K, V, s);
   return hipGetLastError();
 }
 template <typename E> hipError_t step(const LinearStep& a, hipStream_t s) {
-  k_step<E><<<(unsigned)(a.P * a.B * a.H), kThreads, 0, s>>>(a);
+  const unsigned n = (unsigned)(a.P * a.B * a.H);
+  if (a.K * a.V <= 1024) k_step<E, 1><<<n, 64, 0, s>>>(a);
+  else k_step<E, 4><<<n, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace linear
 }  // namespace
 
-int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, int64_t element, bool backward) {
+int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, bool backward) {
   using namespace linear;
-  const int64_t wide = backward && V > K ? V : K;
-  const Share share = share_of(P * B * H, T, element == 4 ? chunk_of<float>((int)wide) : kChunk, backward);
+  const Share share = share_of(P * B * H, T, backward);
   if (share.segments == 1) return 0;
   return ((int64_t)share.jobs * share.segments * P * B * H * (K * V + 1) * 4 + 255) / 256 * 256;
 }
