@@ -138,23 +138,25 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
   static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
-  static __device__ inline int row(int i) { return (int)(threadIdx.x + i * 64 * NW) / kAcross; }
-  static __device__ inline int channel(int i) { return (int)(threadIdx.x + i * 64 * NW) % kAcross * kVec; }
+  static __device__ inline int row(int i, int thread = threadIdx.x) { return (thread + i * 64 * NW) / kAcross; }
+  static __device__ inline int channel(int i, int thread = threadIdx.x) { return (thread + i * 64 * NW) % kAcross * kVec; }
+  static __device__ inline int thread() { return HOW == kWide ? (int)threadIdx.x : here_only(threadIdx.x); }
   __device__ inline void load(const Steps<E, C, HOW>& a, int n, bool reverse) {
     const auto r = a.chunk(n);
+    const int id = thread();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int m = reverse ? C - 1 - row(i) : row(i);
+      const int m = reverse ? C - 1 - row(i, id) : row(i, id);
       if constexpr (HOW == kWide) {
-        v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, a.offset(m, channel(i)), 0, 0);
+        v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, a.offset(m, channel(i, id)), 0, 0);
       } else {
         if (HOW == kNarrow && a.width >= kVec) {                     // in front of the end of an existing row, whatever is asked for
-          const unsigned at = (unsigned)(min(m, n - 1) * (int)a.step + min(channel(i), a.width - kVec));
+          const unsigned at = (unsigned)(min(m, n - 1) * (int)a.step + min(channel(i, id), a.width - kVec));
           __builtin_memcpy(&v[i], a.now + at, 16);
         } else {
           E e[kVec];
 #pragma unroll
-          for (int k = 0; k < kVec; ++k) e[k] = a.element(r, n, m, channel(i) + k);
+          for (int k = 0; k < kVec; ++k) e[k] = a.element(r, n, m, channel(i, id) + k);
           __builtin_memcpy(&v[i], e, 16);
         }
       }
@@ -163,9 +165,10 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   // What was asked for: values of the vector moved to their places, zeros behind the ends of rows and behind the last one.
   __device__ inline void settle(const Steps<E, C, HOW>& a, int n, bool reverse) {
     if (HOW != kNarrow || a.width < kVec) return;
+    const int id = thread();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int m = reverse ? C - 1 - row(i) : row(i), off = max(0, channel(i) - (a.width - kVec)) * (int)sizeof(E) * 8;
+      const int m = reverse ? C - 1 - row(i, id) : row(i, id), off = max(0, channel(i, id) - (a.width - kVec)) * (int)sizeof(E) * 8;
       uint64_t lo = v[i][0] | (uint64_t)v[i][1] << 32, hi = v[i][2] | (uint64_t)v[i][3] << 32;
       if (off >= 64) {
         lo = hi;
@@ -261,6 +264,8 @@ __device__ inline float power(float log2_decay, int n) { return __builtin_amdgcn
 __device__ inline bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
 
+template <bool YES> struct Plain { static constexpr bool yes = YES; };
+
 template <typename E, int KB> constexpr int waves_per_simd() { return sizeof(E) == 2 && KB <= 2 ? 3 : 2; }
 
 // A wavefront has 16 of the state's columns, the workgroup those of NW wavefronts.
@@ -289,7 +294,6 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   const int start = from * C, end = min(until * C, a.T), n_chunks = max(0, (min(end, len) - start + C - 1) / C);
   const int first_t = start + (reverse ? max(n_chunks - 1, 0) * C : 0);
   Array q(role.q, p, b, h, K, first_t, reverse), k(role.k, p, b, h, K, first_t, reverse), v(role.v, p, b, h, V, first_t, reverse), o(role.o, p, b, h, V, first_t, reverse);
-  const int column = 16 * wave + at;
   const bool idle = 16 * wave >= V;                                  // a wave with no columns loads with the others
 
   // the state: S[d][i] is channel channel_of(d, g, i) of this lane's column
@@ -305,6 +309,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
       along_k = job == 2 ? 1 : V;
       along_v = job == 2 ? K : 1;
     }
+    const int g = here_only(lane) >> 4, column = 16 * wave + (here_only(lane) & 15);
 #pragma unroll
     for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
@@ -348,10 +353,12 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   };
   if (n_chunks > 0) load(0);
   if (threadIdx.x == 0) bad[0] = 0;
-  if (n_chunks > 0) sync_lds();
+  sync_lds();
+  if (tainted) bad[0] = 1;
   bool any_cut = false;
 
-  for (int n = 0; n < n_chunks; ++n) {
+  int n = 0;
+  for (; n < n_chunks; ++n) {
     const int t = start + (reverse ? n_chunks - 1 - n : n) * C, count = min(C, len - t);
     if (n > 0) o.now += o.hop;
     const unsigned cuts = (unsigned)__builtin_amdgcn_ballot_w64(next_cut != 0);
@@ -383,22 +390,26 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
-    const bool slow = __builtin_amdgcn_readfirstlane(bad[n & 1]) != 0 || tainted;
+    const int not_fine = bad[n & 1];
     if (threadIdx.x == 0) bad[(n + 1) & 1] = 0;
 
-    if (!states) {
+    f32x4 out[2];                                                    // rows: columns 4 g + i of the wave's; column: row `at` of the tile
+    Operand<kIn> value;
+    const auto pairs = [&](auto plain) {
       // the weights of pairs of rows, for all wavefronts: tiles 0 and 1 with themselves, 1 with 0
       for (int w = NW - 1 - wave; w < 3; w += NW) {
         const int queried = w > 0, other = w == 1;
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int d = 0; d < KB; ++d) x = product(T::rows(keys, other, d, lane), T::rows(queries, queried, d, lane), x);
+        if (w < 2) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (w < 2) x[j] = 4 * g + j <= at ? x[j] * here[j] : 0.0f;
-          else x[j] *= there[j];
+          for (int j = 0; j < 4; ++j) x[j] = 4 * g + j <= at ? x[j] * here[j] : 0.0f;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] *= there[j];
         }
-        if (!regular) {
+        if constexpr (!plain.yes) {
           const int mine = starts(16 * queried + at);
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[j] = starts(16 * other + 4 * g + j) == mine ? x[j] : 0.0f;
@@ -409,77 +420,65 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
 #pragma unroll
         for (int n = 0; n < kOf; ++n) shared_weights[w][n][lane] = u32x2{lo[n], hi[n]};
       }
-    }
-
-    f32x4 out[2];                                                    // rows: columns 4 g + i of the wave's; column: row `at` of the tile
-    Operand<kIn> value;
-    if (idle) {
-    } else if (__builtin_expect(slow, 0)) {
-      // something here is not finite, and a product with a weight of zero would carry it where it does not belong: step by step
-      tainted = false;
-      const E *qs = linear::at<E>(role.q, p, b, h), *ks = linear::at<E>(role.k, p, b, h), *vs = linear::at<E>(role.v, p, b, h);
-      E* os = (E*)linear::at<E>(role.o, p, b, h);
-      const int g = here_only(lane >> 4), column = 16 * wave + here_only(lane & 15);
-#pragma unroll 1
-      for (int r = reverse ? C - count : 0; r < (reverse ? C : count); ++r) {
-        const int64_t s = t + (reverse ? C - 1 - r : r);
-        const bool cut = cuts >> r & 1;
-        const float vr = column < V ? (float)vs[s * role.v.step + column] * role.write : 0.0f;
-        float sum = 0.0f;
+    };
+    const auto from_state = [&](auto plain) {
+      Operand<kOf> memory[KB];
+#pragma unroll
+      for (int d = 0; d < KB; ++d) memory[d] = operand<kOf>(S[2 * d], S[2 * d + 1]);
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) out[tile] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int d = 0; d < KB; ++d)
+#pragma unroll
+        for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::rows(queries, tile, d, lane), out[tile]);
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        float f = into[tile];
+        if constexpr (!plain.yes) {
+          if (reverse) f = role.read * power(l2, max(16 * tile + here_only(at) - (C - count), 0));
+        }
+        out[tile] *= f;
+        if constexpr (!plain.yes) {
+          const bool own = starts(16 * tile + at) != 0;              // nothing of the state
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[tile][e] = own ? 0.0f : out[tile][e];
+        }
+      }
+    };
+    const auto next_state = [&](auto plain) {
+      if constexpr (!plain.yes) {
+        const float keep = power(l2, count);
 #pragma unroll
         for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int kr = channel_of(d, g, i);
-            if (kr < K) {
-              const float x = fmaf((float)ks[s * role.k.step + kr], vr, cut ? 0.0f : reverse ? S[d][i] : lambda * S[d][i]);
-              if (!states) sum = fmaf((float)qs[s * role.q.step + kr], x, sum);
-              S[d][i] = reverse ? lambda * x : x;
-            }
-          }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (!states && g == 0 && column < V) os[s * role.o.step + column] = (E)(sum * role.read);
+          for (int i = 0; i < 4; ++i) S[d][i] = all_starts == 0 ? S[d][i] * keep : 0.0f;
+      } else {
+#pragma unroll
+        for (int d = 0; d < 2 * KB; ++d) S[d] *= whole;
       }
 #pragma unroll
-      for (int d = 0; d < 2 * KB; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tainted |= not_finite(S[d][i]);
-      tainted = any_lane(tainted);
-    } else {
+      for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::channels(faded, d, lane), value, S[d]);
+    };
+    if (!states) {
+      if (regular) pairs(Plain<true>());
+      else pairs(Plain<false>());
+      if (!idle) {
+        if (regular) from_state(Plain<true>());
+        else from_state(Plain<false>());
+      }
+    }
+    // A product with a weight of zero would carry what is not finite where it does not belong: the rest goes step by step.
+    if (__builtin_amdgcn_readfirstlane(not_fine) != 0) break;
+    if (!idle) {
       value = TV::columns(values, wave, lane);
-      if (!states) {
-        Operand<kOf> memory[KB];
-#pragma unroll
-        for (int d = 0; d < KB; ++d) memory[d] = operand<kOf>(S[2 * d], S[2 * d + 1]);
-#pragma unroll
-        for (int tile = 0; tile < 2; ++tile) {
-          out[tile] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int d = 0; d < KB; ++d) out[tile] = product(memory[d], T::rows(queries, tile, d, lane), out[tile]);
-          float f = into[tile];
-          if (!regular && reverse) f = role.read * power(l2, max(16 * tile + here_only(at) - (C - count), 0));
-          out[tile] *= f;
-          if (all_starts != 0) {
-            const bool own = starts(16 * tile + at) != 0;            // nothing of the state
-#pragma unroll
-            for (int e = 0; e < 4; ++e) out[tile][e] = own ? 0.0f : out[tile][e];
-          }
-        }
-      }
-      float keep = whole;
-      if (!regular) keep = power(l2, count);
-      if (all_starts != 0) {
-#pragma unroll
-        for (int d = 0; d < 2 * KB; ++d) S[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-#pragma unroll
-      for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::channels(faded, d, lane), value, S[d] * keep);
+      if (regular) next_state(Plain<true>());
+      else next_state(Plain<false>());
     }
     sync_lds();                                                      // all of the chunk has been read but the weights, which are written
 
-    if (states || idle || slow) continue;
+    if (states || idle) continue;
     const auto r = o.chunk(count);
+    const int id = HOW == kWide ? lane : here_only(lane);
 #pragma unroll
     for (int tile = 0; tile < 2; ++tile) {
       Operand<kOf> weights;
@@ -491,7 +490,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
       const f32x4 y = product(value, weights, out[tile]);
       typedef E Four __attribute__((ext_vector_type(4)));
       const Four x = {(E)y[0], (E)y[1], (E)y[2], (E)y[3]};
-      const int i = 16 * tile + at, m = reverse ? C - 1 - i : i, column = 16 * wave + 4 * g;
+      const int i = 16 * tile + (id & 15), m = reverse ? C - 1 - i : i, column = 16 * wave + 4 * (id >> 4);
       if constexpr (HOW == kWide) {
         if constexpr (sizeof(E) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), r, o.offset(m, column), 0, 0);
         else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, x), r, o.offset(m, column), 0, 0);
@@ -509,8 +508,38 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     }
   }
 
+  if (n < n_chunks && !idle) {
+    const int first = start + (reverse ? 0 : n * C), behind = reverse ? start + min((n_chunks - n) * C, len - start) : min(end, len);
+    const E *qs = linear::at<E>(role.q, p, b, h), *ks = linear::at<E>(role.k, p, b, h), *vs = linear::at<E>(role.v, p, b, h);
+    E* os = (E*)linear::at<E>(role.o, p, b, h);
+    const int g = here_only(lane) >> 4, column = 16 * wave + (here_only(lane) & 15);
+#pragma unroll 1
+    for (int i = first; i < behind; ++i) {
+      const int64_t s = reverse ? first + behind - 1 - i : i;
+      const bool cut = reset && (!reverse || s + 1 < len) && reset[(s + (reverse ? 1 : 0)) * a.reset.step];
+      any_cut |= cut;
+      const float vr = column < V ? (float)vs[s * role.v.step + column] * role.write : 0.0f;
+      float sum = 0.0f;
+#pragma unroll
+      for (int d = 0; d < 2 * KB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int kr = channel_of(d, g, i);
+          if (kr < K) {
+            const float x = fmaf((float)ks[s * role.k.step + kr], vr, cut ? 0.0f : reverse ? S[d][i] : lambda * S[d][i]);
+            if (!states) sum = fmaf((float)qs[s * role.q.step + kr], x, sum);
+            S[d][i] = reverse ? lambda * x : x;
+          }
+        }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (!states && g == 0 && column < V) os[s * role.o.step + column] = (E)(sum * role.read);
+    }
+  }
+
+  const int behind_g = here_only(lane) >> 4, column = 16 * wave + (here_only(lane) & 15);
   if (!states && column < V)
-    for (int t = max(start, len) + g; t < end; t += 4) ((E*)linear::at<E>(role.o, p, b, h))[t * role.o.step + column] = (E)0.0f;
+    for (int t = max(start, len) + behind_g; t < end; t += 4) ((E*)linear::at<E>(role.o, p, b, h))[t * role.o.step + column] = (E)0.0f;
   const bool last = seg == share.segments - 1;
   float* to = states ? ws + (((int64_t)job * share.segments + seg) * cols + col) * K * V : last && role.last ? role.last + (int64_t)col * K * V : nullptr;
   if (!to) return;
@@ -519,7 +548,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   for (int d = 0; d < 2 * KB; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row_k = channel_of(d, g, i);
+      const int row_k = channel_of(d, behind_g, i);
       if (row_k < K && column < V) to[row_k * V + column] = cut ? 0.0f : S[d][i];
     }
   if (states && threadIdx.x == 0) {
