@@ -27,9 +27,10 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 // Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them), a computed operand (a weight, a state, a
 // value times its decay) to 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11.
-template <typename E> struct Parts { static constexpr int kIn = 2, kOf = 2; };
-template <> struct Parts<__bf16> { static constexpr int kIn = 1, kOf = 2; };
-template <> struct Parts<float> { static constexpr int kIn = 3, kOf = 3; };
+// Products of two arrays' values take them as they are where there are instructions for the type: kRaw parts.
+template <typename E> struct Parts { static constexpr int kIn = 2, kOf = 2, kRaw = 1; };
+template <> struct Parts<__bf16> { static constexpr int kIn = 1, kOf = 2, kRaw = 1; };
+template <> struct Parts<float> { static constexpr int kIn = 3, kOf = 3, kRaw = 3; };
 
 // An operand of v_mfma_f32_16x16x32_bf16: lane l has row (or column) l % 16 and the 8 places 4 g + j and 16 + 4 g + j, j = 0 .. 3, g = l / 16,
 // of the 32 that are summed over.  Their order is free as long as both operands have the same, and in this one two results one under the
@@ -74,6 +75,12 @@ template <int A, int B> __device__ inline f32x4 product(const Operand<A>& a, con
       if (n - i >= 0 && n - i < B)
         c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.part[i]), __builtin_bit_cast(bf16x8, b.part[n - i]), c, 0, 0, 0);
   return c;
+}
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <typename E, int N> __device__ inline f32x4 product_of_values(const Operand<N>& a, const Operand<N>& b, f32x4 c) {
+  if constexpr (__is_same(E, _Float16)) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.part[0]), __builtin_bit_cast(f16x8, b.part[0]), c, 0, 0, 0);
+  else return product(a, b, c);
 }
 
 __device__ inline void sync_lds() {
@@ -134,7 +141,7 @@ __device__ inline int channel_of(int d, int g, int i) { return 32 * (d / 2) + 8 
 // end in reverse.
 template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   static constexpr int kVec = 16 / sizeof(E), kAcross = 32 * KB / kVec, kAll = C * kAcross, kEach = (kAll + 64 * NW - 1) / (64 * NW);
-  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kPairs = kVec / 2;
+  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
   typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
   static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
@@ -183,18 +190,19 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   }
   __device__ inline bool finite() const {
     unsigned bad = 0;
+    float zero = 0.0f;                                               // but where a value is not finite
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (!whole(i)) break;
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const unsigned w = v[i][d];
-        if constexpr (sizeof(E) == 4) bad |= (w & 0x7f800000u) + 0x00800000u;
+        if constexpr (sizeof(E) == 4) zero = fmaf(__uint_as_float(w), 0.0f, zero);
         else if constexpr (kIn == 1) bad |= (w & 0x7f807f80u) + 0x00800080u;
         else bad |= (w & 0x7c007c00u) + 0x04000400u;
       }
     }
-    return (bad & (sizeof(E) == 4 ? 0x80000000u : 0x80008000u)) == 0;
+    return sizeof(E) == 4 ? zero == 0.0f : (bad & 0x80008000u) == 0;
   }
   __device__ inline void pair(int i, int d, float& a, float& b) const {
     if constexpr (sizeof(E) == 4) {
@@ -209,13 +217,13 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     }
   }
   static __device__ inline unsigned short* place(unsigned short* plane, int i) { return plane + row(i) * kStride + channel(i); }
-  // Into LDS, part by part.
-  __device__ inline void store(unsigned short* plane) const {
+  // Into LDS, part by part, or as they are.
+  template <int N> __device__ inline void store(unsigned short* plane) const {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (!whole(i)) break;
-      if constexpr (kIn == 1) *(u32x4*)place(plane, i) = v[i];
-      else put<kIn>(plane, i, 1.0f, false);
+      if constexpr (N == 1) *(u32x4*)place(plane, i) = v[i];
+      else put<N>(plane, i, 1.0f, false);
     }
   }
   // Vector i times f.
@@ -235,11 +243,11 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     for (int n = 0; n < N; ++n) *(Word*)(place(plane, i) + n * kPlane) = word[n];
   }
   // Rows 16 tile .. of 32 channels as an operand: a lane has channels 8 g .. 8 g + 7.
-  static __device__ inline Operand<kIn> rows(const unsigned short* plane, int tile, int kb, int lane) {
-    Operand<kIn> o;
+  template <int N> static __device__ inline Operand<N> rows(const unsigned short* plane, int tile, int kb, int lane) {
+    Operand<N> o;
     const unsigned short* from = plane + (16 * tile + (lane & 15)) * kStride + 32 * kb + 8 * (lane >> 4);
 #pragma unroll
-    for (int n = 0; n < kIn; ++n) o.part[n] = *(const u32x4*)(from + n * kPlane);
+    for (int n = 0; n < N; ++n) o.part[n] = *(const u32x4*)(from + n * kPlane);
     return o;
   }
   // Sixteen channels of 32 rows as an operand, four rows of four times four channels turned over by the read: those of half `d % 2` of block
@@ -266,7 +274,7 @@ __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) 
 
 template <bool YES> struct Plain { static constexpr bool yes = YES; };
 
-template <typename E, int KB> constexpr int waves_per_simd() { return sizeof(E) == 2 && KB <= 2 ? 3 : 2; }
+template <typename E, int KB> constexpr int waves_per_simd() { return KB > 2 ? 2 : sizeof(E) == 4 ? (KB == 1 ? 3 : 2) : __is_same(E, __bf16) || KB == 1 ? 4 : 3; }
 
 // A wavefront has 16 of the state's columns, the workgroup those of NW wavefronts.
 template <typename E, int KB, int NW, int C, int HOW>
@@ -274,9 +282,10 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   typedef Tile<E, KB, NW, C, HOW> T;
   typedef Tile<E, NW / 2, NW, C, HOW> TV;
   typedef Steps<E, C, HOW> Array;
-  constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf;
+  constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw;
+  constexpr bool kTwice = kIn != kRaw;                               // queries in parts and as they are
   static_assert(C == 32, "two tiles of rows; starts of episodes are the bits of a word");
-  __shared__ __attribute__((aligned(16))) unsigned short keys[kIn * T::kPlane], queries[kIn * T::kPlane], faded[kOf * T::kPlane], values[kIn * TV::kPlane];
+  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kOf * T::kPlane], values[kIn * TV::kPlane];
   __shared__ u32x2 shared_weights[3][kOf][64];
   __shared__ int bad[2];
   // the roles of a column one after the other on one XCD: they read the same arrays
@@ -321,15 +330,9 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     tainted = any_lane(tainted);
   }
 
-  // Weights of pairs, row `at` of a tile and row 4 g + j of the same one, or of the one in front.  Weights of the state on its way in, and of
-  // this thread's rows of keys on their way out.
+  // Weights of the state on its way in, and of this thread's rows of keys on their way out.
   const float both = role.read * role.write, whole = power(l2, C);
-  float here[4], there[4], into[2], outof[T::kEach];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    here[j] = both * power(l2, max(at - 4 * g - j, 0));
-    there[j] = both * power(l2, 16 + at - 4 * g - j);
-  }
+  float into[2], outof[T::kEach];
 #pragma unroll
   for (int n = 0; n < 2; ++n) into[n] = role.read * power(l2, 16 * n + at + before);
 #pragma unroll
@@ -368,12 +371,13 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     const int all_starts = __popc(cuts);
     next_k.settle(k, count, reverse);
     next_v.settle(v, count, reverse);
-    next_v.store(values);
+    next_v.template store<kIn>(values);
     bool fine = next_k.finite() & next_v.finite();
     if (!states) {
       next_q.settle(q, count, reverse);
-      next_k.store(keys);
-      next_q.store(queries);
+      next_k.template store<kRaw>(keys);
+      next_q.template store<kIn>(queries);
+      if constexpr (kTwice) next_q.template store<kRaw>(asked);
       fine &= next_q.finite();
     }
     if (!fine) bad[n & 1] = 1;
@@ -401,14 +405,11 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         const int queried = w > 0, other = w == 1;
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int d = 0; d < KB; ++d) x = product(T::rows(keys, other, d, lane), T::rows(queries, queried, d, lane), x);
-        if (w < 2) {
+        for (int d = 0; d < KB; ++d) x = product_of_values<E>(T::template rows<kRaw>(keys, other, d, lane), T::template rows<kRaw>(kTwice ? asked : queries, queried, d, lane), x);
+        // row `at` of the one and row 4 g + j of the other
+        const int first = here_only(at - 4 * g) + (w < 2 ? 0 : 16);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = 4 * g + j <= at ? x[j] * here[j] : 0.0f;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] *= there[j];
-        }
+        for (int j = 0; j < 4; ++j) x[j] = first >= j ? x[j] * (both * power(l2, first - j)) : 0.0f;
         if constexpr (!plain.yes) {
           const int mine = starts(16 * queried + at);
 #pragma unroll
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
 #pragma unroll
       for (int d = 0; d < KB; ++d)
 #pragma unroll
-        for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::rows(queries, tile, d, lane), out[tile]);
+        for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::template rows<kIn>(queries, tile, d, lane), out[tile]);
 #pragma unroll
       for (int tile = 0; tile < 2; ++tile) {
         float f = into[tile];
@@ -656,11 +657,30 @@ template <typename E, int NW> __global__ void __launch_bounds__(64 * NW) k_step(
   }
 }
 
-// Sequences are cut into segments where there are too few of them: the segments' own states first, then those in front of them.
-constexpr int kChunk = 32, kWorkgroups = 1024, kLeast = 4, kMostSegments = 4096;
-Share share_of(int64_t cols, int64_t T, bool backward) {
+constexpr int kChunk = 32, kLeast = 4, kMostSegments = 4096, kCUs = 256, kLds = 160 << 10;
+int blocks_of(int K) { return K <= 32 ? 1 : K <= 64 ? 2 : 4; }
+int waves_of(int V) { return V <= 32 ? 2 : V <= 64 ? 4 : 8; }
+
+// Workgroups that the card holds at once.
+template <typename E, int KB> int64_t at_once(int waves) {
+  typedef Parts<E> P;
+  const int plane = 2 * kChunk * (32 * KB + 8), values = 2 * kChunk * (16 * waves + 8);
+  const int lds = (P::kRaw + P::kIn + P::kOf + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
+  const int by_lds = kLds / lds, by_waves = 4 * waves_per_simd<E, KB>() / waves;
+  return (int64_t)kCUs * (by_lds < by_waves ? by_lds : by_waves);
+}
+template <typename E> int64_t at_once(int K, int V) {
+  const int kb = blocks_of(K), waves = waves_of(V);
+  return kb == 1 ? at_once<E, 1>(waves) : kb == 2 ? at_once<E, 2>(waves) : at_once<E, 4>(waves);
+}
+
+// Sequences are cut into segments where there are too few of them, the segments' own states first, then those in front of them: as many as
+// one round of workgroups takes.  Roles go together, in a kernel that is wide enough for all.
+Share share_of(int64_t cols, int64_t T, int K, int V, int dtype, bool backward) {
   const int64_t chunks = (T + kChunk - 1) / kChunk, roles = backward ? 3 : 1;
-  int64_t want = kWorkgroups / (cols * roles);
+  if (backward) K = V = K > V ? K : V;
+  const int64_t slots = dtype == POP_F32 ? at_once<float>(K, V) : dtype == POP_BF16 ? at_once<__bf16>(K, V) : at_once<_Float16>(K, V);
+  int64_t want = slots / (cols * roles);
   if (want > kMostSegments) want = kMostSegments;
   if (want > chunks / kLeast) want = chunks / kLeast;
   if (want <= 1) return {(int)chunks, (int)chunks, 1, 0};
@@ -670,17 +690,16 @@ Share share_of(int64_t cols, int64_t T, bool backward) {
 
 typedef void (*Kernel)(LinearArgs, Share, float*, int, int);
 template <typename E, int KB, int HOW> Kernel kernel_of(int V) {
-  return V > 64 ? k_chunks<E, KB, 8, kChunk, HOW> : V > 32 ? k_chunks<E, KB, 4, kChunk, HOW> : k_chunks<E, KB, 2, kChunk, HOW>;
+  return waves_of(V) == 8 ? k_chunks<E, KB, 8, kChunk, HOW> : waves_of(V) == 4 ? k_chunks<E, KB, 4, kChunk, HOW> : k_chunks<E, KB, 2, kChunk, HOW>;
 }
 template <typename E, int HOW> Kernel kernel_of(int K, int V) {
-  return K <= 32 ? kernel_of<E, 1, HOW>(V) : K <= 64 ? kernel_of<E, 2, HOW>(V) : kernel_of<E, 4, HOW>(V);
+  return blocks_of(K) == 1 ? kernel_of<E, 1, HOW>(V) : blocks_of(K) == 2 ? kernel_of<E, 2, HOW>(V) : kernel_of<E, 4, HOW>(V);
 }
 template <typename E> void launch(int how, const LinearArgs& a, const Share& share, float* ws, int mode, int jobs, int K, int V, hipStream_t s) {
-  constexpr int kAll = POP_LINEAR_MAX_DIM;
-  const Kernel k = how == kWide ? kernel_of<E, kWide>(K, V) : how == kNarrow ? kernel_of<E, kNarrow>(K, V) : k_chunks<E, kAll / 32, kAll / 16, kChunk, kAny>;
-  const int waves = how == kAny || V > 64 ? 8 : V > 32 ? 4 : 2;
+  if (how == kAny) K = V = POP_LINEAR_MAX_DIM;
+  const Kernel k = how == kWide ? kernel_of<E, kWide>(K, V) : how == kNarrow ? kernel_of<E, kNarrow>(K, V) : k_chunks<E, POP_LINEAR_MAX_DIM / 32, 8, kChunk, kAny>;
   const unsigned cols = (unsigned)(a.P * a.B * a.H);
-  k<<<(cols * share.segments + 7) / 8 * 8 * jobs, 64 * waves, 0, s>>>(a, share, ws, mode, jobs);
+  k<<<(cols * share.segments + 7) / 8 * 8 * jobs, 64 * waves_of(V), 0, s>>>(a, share, ws, mode, jobs);
 }
 template <typename E> int how_of(const LinearArgs& a) {
   int how = kWide;
@@ -696,10 +715,9 @@ template <typename E> int how_of(const LinearArgs& a) {
   }
   return how;
 }
-template <typename E> hipError_t run(const LinearArgs& a, float* ws, hipStream_t s) {
+template <typename E> hipError_t run(const LinearArgs& a, int dtype, float* ws, hipStream_t s) {
   const int cols = a.P * a.B * a.H;
-  const Share share = share_of(cols, a.T, a.roles > 1);
-  // roles go together, in a kernel that is wide enough for all
+  const Share share = share_of(cols, a.T, a.role[0].K, a.role[0].V, dtype, a.roles > 1);
   const int most = a.role[0].K > a.role[0].V ? a.role[0].K : a.role[0].V, K = a.roles > 1 ? most : a.role[0].K, V = a.roles > 1 ? most : a.role[0].V;
   const int how = how_of<E>(a);
   if (share.segments > 1) {
@@ -721,15 +739,15 @@ template <typename E> hipError_t step(const LinearStep& a, hipStream_t s) {
 }  // namespace linear
 }  // namespace
 
-int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, bool backward) {
+int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, int dtype, bool backward) {
   using namespace linear;
-  const Share share = share_of(P * B * H, T, backward);
+  const Share share = share_of(P * B * H, T, (int)K, (int)V, dtype, backward);
   if (share.segments == 1) return 0;
   return ((int64_t)share.jobs * share.segments * P * B * H * (K * V + 1) * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_linear(const LinearArgs& a, int dtype, void* ws, hipStream_t s) {
-  return dtype == POP_F32 ? linear::run<float>(a, (float*)ws, s) : dtype == POP_BF16 ? linear::run<__bf16>(a, (float*)ws, s) : linear::run<_Float16>(a, (float*)ws, s);
+  return dtype == POP_F32 ? linear::run<float>(a, dtype, (float*)ws, s) : dtype == POP_BF16 ? linear::run<__bf16>(a, dtype, (float*)ws, s) : linear::run<_Float16>(a, dtype, (float*)ws, s);
 }
 hipError_t launch_linear_step(const LinearStep& a, int dtype, hipStream_t s) {
   return dtype == POP_F32 ? linear::step<float>(a, s) : dtype == POP_BF16 ? linear::step<__bf16>(a, s) : linear::step<_Float16>(a, s);

@@ -280,7 +280,7 @@ LinearArgs linear_args(const pop_linear_config* c, const pop_linear_io* io) {
 
 int64_t linear_workspace(const pop_linear_config* c, bool backward) {
   const int rc = check_linear(c);
-  return rc != POP_OK ? rc : linear_workspace_bytes(c->P, c->batch, c->T, c->heads, c->key_dim, c->value_dim, backward);
+  return rc != POP_OK ? rc : linear_workspace_bytes(c->P, c->batch, c->T, c->heads, c->key_dim, c->value_dim, c->dtype, backward);
 }
 
 // ---- clipping

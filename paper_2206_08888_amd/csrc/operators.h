@@ -68,7 +68,7 @@ struct LinearStep {
   int n_slots;
   const int32_t* slots;
 };
-int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, bool backward);
+int64_t linear_workspace_bytes(int64_t P, int64_t B, int64_t T, int64_t H, int64_t K, int64_t V, int dtype, bool backward);
 hipError_t launch_linear(const LinearArgs& a, int dtype, void* ws, hipStream_t s);
 hipError_t launch_linear_step(const LinearStep& a, int dtype, hipStream_t s);
 
