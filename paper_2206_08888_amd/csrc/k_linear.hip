@@ -559,18 +559,22 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
 }
 
 // The states in front of the segments, in the places of what the segments add to them.  A negative factor: nothing of the state in front
-// is left.
+// is left.  A workgroup has 64 elements of states, a wavefront AHEAD segments in a row: it finds what they do together, and with
+// what those of the wavefronts in front do the states in front of each.  (192 segments of 4 states of 64 x 64, one after the other: 17 us.)
 constexpr int kScan = 64;
-template <int AHEAD> __global__ void __launch_bounds__(kScan) k_scan(LinearArgs a, Share share, float* ws, int cols) {
+template <int NW, int AHEAD> __global__ void __launch_bounds__(kScan * NW) k_scan(LinearArgs a, Share share, float* ws, int cols) {
+  __shared__ float sums[NW][kScan], factors[NW][kScan];
   const LinearRole& role = a.role[blockIdx.y];
-  const int size = role.K * role.V, n = cols * size, i = blockIdx.x * kScan + threadIdx.x;    // few columns: n is below 2^24
-  if (i >= n) return;
-  const int col = i / size, e = i - col * size;
+  const int size = role.K * role.V, n = cols * size, lane = threadIdx.x % kScan, wave = threadIdx.x / kScan;     // few columns: n is below 2^27
+  const int i = min(blockIdx.x * kScan + lane, n - 1), col = i / size, e = i - col * size;
+  const bool mine = blockIdx.x * kScan + lane < n;
   float* at = ws + (int64_t)blockIdx.y * share.segments * n + i;
   const float* factor = ws + (int64_t)share.jobs * share.segments * n + (int64_t)blockIdx.y * share.segments * cols + col;
+  const auto behind = [](float s, float sum, float f) { return f < 0.0f ? sum : fmaf(f, s, sum); };
   float s = role.first ? role.first[(int64_t)col * size + e / role.V * role.first_k + e % role.V * role.first_v] : 0.0f;
-  for (int k = 0; k < share.segments; k += AHEAD) {
-    float add[AHEAD], f[AHEAD];
+  for (int all = 0; all < share.segments; all += NW * AHEAD) {
+    const int k = all + wave * AHEAD;
+    float add[AHEAD], f[AHEAD], sum = 0.0f, product = 1.0f;
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int from = min(k + u, share.segments - 1);
@@ -579,9 +583,32 @@ template <int AHEAD> __global__ void __launch_bounds__(kScan) k_scan(LinearArgs 
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      if (k + u >= share.segments) break;
-      at[(int64_t)(k + u) * n] = s;
-      s = f[u] < 0.0f ? add[u] : fmaf(f[u], s, add[u]);
+      if (k + u >= share.segments) continue;
+      sum = behind(sum, add[u], f[u]);
+      product = f[u] < 0.0f || product < 0.0f ? -1.0f : product * f[u];
+    }
+    if (NW > 1) {
+      sums[wave][lane] = sum;
+      factors[wave][lane] = product;
+      __syncthreads();
+      float in_front = s;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        if (w == wave) in_front = s;
+        s = behind(s, sums[w][lane], factors[w][lane]);
+      }
+      if (all + NW * AHEAD < share.segments) __syncthreads();
+      sum = in_front;
+    } else {
+      const float in_front = s;
+      s = behind(s, sum, product);
+      sum = in_front;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k + u >= share.segments) continue;
+      if (mine) at[(int64_t)(k + u) * n] = sum;
+      sum = behind(sum, add[u], f[u]);
     }
   }
 }
@@ -674,18 +701,31 @@ template <typename E> int64_t at_once(int K, int V) {
   return kb == 1 ? at_once<E, 1>(waves) : kb == 2 ? at_once<E, 2>(waves) : at_once<E, 4>(waves);
 }
 
-// Sequences are cut into segments where there are too few of them, the segments' own states first, then those in front of them: as many as
-// one round of workgroups takes.  Roles go together, in a kernel that is wide enough for all.
+// Sequences are cut into segments where there are too few of them, the segments' own states first, then those in front of them.  Roles go
+// together, in a kernel that is wide enough for all.  Of the numbers of segments that fill whole rounds of workgroups, the one whose
+// chunks one after the other take least: a chunk of states takes about half as long as one with outputs (28 / 50 us for 10 x 4 x 1000 x 4
+// heads of 64, fp32), a workgroup's beginning and end as long as two chunks, the two launches more as long as two with outputs, the scan
+// a fortieth of one for each segment.
 Share share_of(int64_t cols, int64_t T, int K, int V, int dtype, bool backward) {
-  const int64_t chunks = (T + kChunk - 1) / kChunk, roles = backward ? 3 : 1;
+  const int64_t chunks = (T + kChunk - 1) / kChunk, roles = backward ? 3 : 1, jobs = backward ? 2 : 1;
   if (backward) K = V = K > V ? K : V;
   const int64_t slots = dtype == POP_F32 ? at_once<float>(K, V) : dtype == POP_BF16 ? at_once<__bf16>(K, V) : at_once<_Float16>(K, V);
-  int64_t want = slots / (cols * roles);
-  if (want > kMostSegments) want = kMostSegments;
-  if (want > chunks / kLeast) want = chunks / kLeast;
-  if (want <= 1) return {(int)chunks, (int)chunks, 1, 0};
-  const int64_t per = (chunks + want - 1) / want;
-  return {(int)chunks, (int)per, (int)((chunks + per - 1) / per), backward ? 2 : 1};
+  const auto rounds = [&](int64_t workgroups) { return (workgroups + slots - 1) / slots; };
+  Share best = {(int)chunks, (int)chunks, 1, 0};
+  int64_t least = 40 * (chunks + 2) * rounds(cols * roles);
+  for (int n = 1; n <= 8; ++n)
+    for (int64_t each : {cols * roles, cols * jobs}) {
+      int64_t want = n * slots / each;
+      if (want > kMostSegments) want = kMostSegments;
+      if (want > chunks / kLeast) want = chunks / kLeast;
+      if (want <= 1) continue;
+      const int64_t per = (chunks + want - 1) / want, segments = (chunks + per - 1) / per;
+      const int64_t cost = (per + 2) * (40 * rounds(cols * roles * segments) + 20 * rounds(cols * jobs * segments)) + 80 + segments;
+      if (cost >= least) continue;
+      least = cost;
+      best = {(int)chunks, (int)per, (int)segments, (int)jobs};
+    }
+  return best;
 }
 
 typedef void (*Kernel)(LinearArgs, Share, float*, int, int);
@@ -723,8 +763,11 @@ template <typename E> hipError_t run(const LinearArgs& a, int dtype, float* ws, 
   if (share.segments > 1) {
     launch<E>(how, a, share, ws, kStates, share.jobs, K, V, s);
     const dim3 grid((cols * a.role[0].K * a.role[0].V + kScan - 1) / kScan, share.jobs);
-    if (share.segments <= 8) k_scan<4><<<grid, kScan, 0, s>>>(a, share, ws, cols);
-    else k_scan<16><<<grid, kScan, 0, s>>>(a, share, ws, cols);
+    const auto scan = [&](auto kernel, int waves) { kernel<<<grid, kScan * waves, 0, s>>>(a, share, ws, cols); };
+    if (share.segments <= 4) scan(k_scan<1, 4>, 1);
+    else if (share.segments <= 16) scan(k_scan<4, 4>, 4);
+    else if (share.segments <= 64) scan(k_scan<4, 16>, 4);
+    else scan(k_scan<16, 16>, 16);
   }
   launch<E>(how, a, share, ws, kMain, a.roles, K, V, s);
   return hipGetLastError();
