@@ -274,6 +274,8 @@ __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) 
 
 template <bool YES> struct Plain { static constexpr bool yes = YES; };
 
+constexpr int kGroups = 1 << 15;       // of 8 columns, in x of a grid: its work items stay below 2^32
+
 template <typename E, int KB> constexpr int waves_per_simd() { return KB > 2 ? 2 : sizeof(E) == 4 ? (KB == 1 ? 3 : 2) : __is_same(E, __bf16) || KB == 1 ? 4 : 3; }
 
 // A wavefront has 16 of the state's columns, the workgroup those of NW wavefronts.
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   __shared__ u32x2 shared_weights[3][kOf][64];
   __shared__ int bad[2];
   // the roles of a column one after the other on one XCD: they read the same arrays
-  const int job = blockIdx.x / 8 % jobs, unit = blockIdx.x / (8 * jobs) * 8 + blockIdx.x % 8, cols = a.P * a.B * a.H;
+  const int job = blockIdx.x / 8 % jobs, unit = (blockIdx.y * kGroups + blockIdx.x / (8 * jobs)) * 8 + blockIdx.x % 8, cols = a.P * a.B * a.H;
   if (unit >= cols * share.segments) return;
   const LinearRole& role = a.role[job];
   const int seg = unit / cols, col = unit - seg * cols, h = col % a.H, row = col / a.H, b = row % a.B, p = row / a.B;
@@ -738,8 +740,8 @@ template <typename E, int HOW> Kernel kernel_of(int K, int V) {
 template <typename E> void launch(int how, const LinearArgs& a, const Share& share, float* ws, int mode, int jobs, int K, int V, hipStream_t s) {
   if (how == kAny) K = V = POP_LINEAR_MAX_DIM;
   const Kernel k = how == kWide ? kernel_of<E, kWide>(K, V) : how == kNarrow ? kernel_of<E, kNarrow>(K, V) : k_chunks<E, POP_LINEAR_MAX_DIM / 32, 8, kChunk, kAny>;
-  const unsigned cols = (unsigned)(a.P * a.B * a.H);
-  k<<<(cols * share.segments + 7) / 8 * 8 * jobs, 64 * waves_of(V), 0, s>>>(a, share, ws, mode, jobs);
+  const unsigned groups = (unsigned)((a.P * a.B * a.H * share.segments + 7) / 8), across = groups < kGroups ? groups : kGroups;
+  k<<<dim3(across * 8 * jobs, (groups + across - 1) / across), 64 * waves_of(V), 0, s>>>(a, share, ws, mode, jobs);
 }
 template <typename E> int how_of(const LinearArgs& a) {
   int how = kWide;

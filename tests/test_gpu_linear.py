@@ -248,6 +248,49 @@ def test_last_states_over_first_ones():
         assert torch.equal(o, want[0]) and torch.equal(state, want[1])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K, V", [(7, 9), (8, 16), (9, 100), (66, 30), (127, 65), (128, 24)])
+@pytest.mark.parametrize("layout", ["packed", "time_major"])
+def test_widths_and_segments(K, V, layout, dtype):
+    """Every width of kernel, rows that are not whole vectors, a few sequences in segments."""
+    shape = (1, 2, 700, 2, K, V)
+    c, do, dlast = make(shape, dtype, seed=K, layout=layout, reset=0.004, ragged=True, state0=True, decay=(0.001, 0.1))
+    check_forward(shape, dtype, c)
+    check_backward(shape, dtype, c, do, dlast)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("far", ["step", "over"])
+def test_steps_far_apart_and_over_each_other(far, dtype):
+    """Steps further apart than offsets of 32 bits reach (half of the memory untouched), and one step that all steps share."""
+    shape = (1, 1, 40, 1, 16, 24)
+    c, do, dlast = make(shape, dtype, state0=True)
+    if far == "over":
+        c["k"] = c["k"][:, :, :1].expand(c["k"].shape)
+        c["v"] = c["v"][:, :, 3:4].expand(c["v"].shape)
+    else:
+        size = (1 << 31) // c["q"].element_size() // 40
+        wide = torch.empty((1, 1, 40, size), dtype=dtype, device="cuda")
+        wide[..., :16] = c["q"][:, :, :, 0]
+        c["q"] = wide[..., :16].unflatten(-1, (1, 16))
+    check_forward(shape, dtype, c)
+    check_backward(shape, dtype, c, do, dlast)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_not_finite_in_segments(dtype):
+    """Long sequences in segments: what is not finite in one of them reaches those that follow until an episode starts."""
+    shape = (1, 2, 3000, 1, 16, 20)
+    c, do, dlast = make(shape, dtype, seed=9, decay=(0.0005, 0.01), state0=True)
+    c["reset"] = torch.zeros((1, 2, 3000), dtype=torch.bool, device="cuda")
+    c["reset"][0, 0, 2000] = c["reset"][0, 1, 700] = True
+    c["k"][0, 0, 500, 0, 3] = float("inf")
+    c["v"][0, 1, 1500, 0, 7] = float("nan")
+    do[0, 0, 2500, 0, 2] = float("nan")
+    check_forward(shape, dtype, c)
+    check_backward(shape, dtype, c, do, dlast)
+
+
 @pytest.mark.parametrize("shape", [(2, 2, 150, 2, 32, 32), (1, 1, 5000, 1, 32, 32)])
 def test_captured_and_replayed(shape):
     """A graph of forward, backward and a step, replayed with eager work between; each replay against the eager result."""
@@ -339,3 +382,31 @@ def test_a_state_table_that_is_overwritten_is_seen():
     pp.LinearAttention(1, 1, 1, 1, 4, 4).step(x, x, x, state)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.backward()
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_more_columns_than_a_row_of_the_grid(T):
+    """Five million memories of one number each: o_t = scale q_t sum_s lambda^(t - s) k_s v_s."""
+    B, H = 1 << 20, 5
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    q, k, v, do = (torch.randn((1, B, T, H, 1), generator=gen, device="cuda") for _ in range(4))
+    log = torch.full((1, H), -0.25, device="cuda")
+    plan = pp.LinearAttention(1, B, T, H, 1, 1, scale=0.5)
+    o, last = plan.forward(q, k, v, log)
+    dq, dk, dv, d0 = plan.backward(q, k, v, do, log)
+    lam = torch.exp(torch.tensor(-0.25, dtype=torch.float64))
+    Q, K, V, D = (x.double() for x in (q, k, v, do))
+    S, M = torch.zeros_like(Q[:, :, 0]), torch.zeros_like(Q[:, :, 0])
+    for t in range(T):
+        S, M = lam * S + K[:, :, t] * V[:, :, t], lam * M + (K[:, :, t] * V[:, :, t]).abs()
+        # operands to 2^-23, a dozen roundings of sums and factors
+        for got, want, size in ((o, 0.5 * S * Q[:, :, t], M * Q[:, :, t].abs()), (dq, 0.5 * S * D[:, :, t], M * D[:, :, t].abs())):
+            assert bool(((got[:, :, t] - want).abs() <= 32 * 2.0 ** -24 * size + 1e-37).all())
+    assert bool(((last[..., 0] - S).abs() <= 32 * 2.0 ** -24 * M + 1e-37).all())
+    G, N = torch.zeros_like(S), torch.zeros_like(S)
+    for t in reversed(range(T)):
+        G, N = lam * G + 0.5 * Q[:, :, t] * D[:, :, t], lam * N + (0.5 * Q[:, :, t] * D[:, :, t]).abs()
+        for got, want, size in ((dk, G * V[:, :, t], N * V[:, :, t].abs()), (dv, G * K[:, :, t], N * K[:, :, t].abs())):
+            assert bool(((got[:, :, t] - want).abs() <= 32 * 2.0 ** -24 * size + 1e-37).all())
+    assert bool(((d0[..., 0] - lam * G).abs() <= 32 * 2.0 ** -24 * N + 1e-37).all())
