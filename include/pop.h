@@ -417,7 +417,8 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  *
  * with S_{-1} = state0 and, where reset_t is not zero, 0 in place of S_{t-1}.  Steps from a sequence's length on are not used;
  * o is 0 there and so are the gradients.  States and sums are fp32 whatever the arrays' type.  An infinity or a NaN reaches the steps
- * that the formula lets it reach and no others: not earlier ones, and none behind a reset.
+ * that the formula lets it reach and no others: not earlier ones, and none behind a reset.  Steps are summed in groups, which takes
+ * scale * (k_s . q_t) of steps up to 32 apart: beyond fp32's range it is an infinity even where the state's products are not.
  *
  * POP_EUNSUPPORTED: key_dim or value_dim beyond 128, T beyond 2^22, P * batch * heads from 2^24 on. */
 enum { POP_LINEAR_MAX_DIM = 128 };

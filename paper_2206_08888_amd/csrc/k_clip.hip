@@ -2,8 +2,11 @@
 //
 //   norm = sqrt(sum g^2);  f = 1 where norm + eps <= limit, else limit / (norm + eps);  out = f g
 //
-// Three launches: squares of pieces of kClipPiece elements, a workgroup each; an agent's pieces; the products.  Squares are exact in
-// fp64 and summed there.
+// Squares of pieces of kClipPiece elements, a workgroup each, exact in fp64 and summed there; then the products, whose workgroups sum an
+// agent's pieces for themselves where it has up to kFew, so that two launches do (10 agents of six tensors: 39 -> 28 us a call, most of it the
+// host's), and a launch for the norms in between where it has more.  Bound by memory: gradients are read twice and written once, with
+// the second reading from the end, where it finds in the last cache what was read last: 4 agents of 30 million fp32 elements in 18 tensors,
+// 246 us, 1.45 GB at 5.9 TB/s.  Results past the caches (kPast): 246 against 277 us there.
 #include <hip/hip_runtime.h>
 #include "operators.h"
 
@@ -144,6 +147,7 @@ template <int N> __global__ void __launch_bounds__(kThreads) k_squares(Tensors<N
   if (threadIdx.x == 0) sums[(int64_t)p.agent * pieces_of_all + first + (int)blockIdx.x - p.agent * a.pieces] = all;
 }
 
+// The sums of an agent's pieces, and what becomes of them.
 struct Limits {
   const double* sums;
   int pieces;

@@ -1,6 +1,24 @@
 // Linear attention with a decay for each head over sequences, its backward pass, and single steps (operators.h).
 //
-// HEADER
+// Sequences go in chunks of 32 steps.  With S the state in front of a chunk and i, j its steps from 0 on,
+//
+//   o_i = read (lambda^(i+1) S^T q_i + write sum_{j <= i} lambda^(i-j) (k_j . q_i) v_j),    S' = lambda^32 S + write sum_j lambda^(31-j) k_j v_j^T
+//
+// and where episodes start, pairs of steps in different ones have weight 0 and the state reaches steps in front of the first start only.
+// All sums are products of 16 x 16 x 32 on the bf16 matrix instructions, operands in exact or 16 to 24 bit parts (Parts), sums in fp32.  The
+// three gradients are the same sums with other roles (op_api.hip): dq with d_o, v, k for q, k, v and the states turned over; dv and dk from
+// the end with k, q, d_o and v, d_o, q.  They go in one launch.
+//
+// A workgroup has a column (agent, sequence, head) and walks its chunks: vectors of the next chunk are loaded while this one is computed,
+// split into parts and laid into LDS, keys a second time times their weight in S'; three wavefronts compute the weights of pairs for
+// all; each wavefront holds 16 columns of S in registers, as sums of the matrix instructions that are operands of the next ones as they are.
+// Two barriers a chunk.
+//
+// What bounds it: at 64 x 64 in bf16 memory and the issue of instructions together (80 x 8 x 512 x 4 heads: forward 170 us where the bytes alone
+// take 131 at a large copy's rate, without memory 115 and without sums 160; three gradients 410 us, 230 at least).  At 128 x 128 in fp16 the
+// reads of operands from LDS, 1 KB for each 16 x 16 x 32 product: 720 us, forward and backward of 2 x 2 x 16383 x 4 heads.  fp32 has six
+// products for one, and 60 KB of LDS for a workgroup of 64 x 64: two on a CU.  Chunks of 64 steps need the registers of two; 32 columns a
+// wavefront, which would halve the reads of LDS, do not fit either.
 #include <hip/hip_runtime.h>
 #include "operators.h"
 
@@ -25,9 +43,11 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 #define POP_LDS __attribute__((address_space(3)))
 
-// Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them), a computed operand (a weight, a state, a
-// value times its decay) to 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11.
-// Products of two arrays' values take them as they are where there are instructions for the type: kRaw parts.
+// Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them); a computed operand of outputs (a weight, a state) to
+// 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11 (kOf); keys times their decay to 24 bits (kFaded),
+// as states are fp32.
+// Where both operands are arrays' values, products take them as they are where there are instructions for the type: kRaw parts.
+constexpr int kFaded = 3;
 template <typename E> struct Parts { static constexpr int kIn = 2, kOf = 2, kRaw = 1; };
 template <> struct Parts<__bf16> { static constexpr int kIn = 1, kOf = 2, kRaw = 1; };
 template <> struct Parts<float> { static constexpr int kIn = 3, kOf = 3, kRaw = 3; };
@@ -264,7 +284,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     }
     return o;
   }
-  static __device__ inline Operand<kOf> channels(unsigned short* plane, int d, int lane) { return turned<kOf>(plane, channel_of(d, lane & 3, 0), lane); }
+  static __device__ inline Operand<kFaded> channels(unsigned short* plane, int d, int lane) { return turned<kFaded>(plane, channel_of(d, lane & 3, 0), lane); }
   static __device__ inline Operand<kIn> columns(unsigned short* plane, int w, int lane) { return turned<kIn>(plane, 16 * w + 4 * (lane & 3), lane); }
 };
 
@@ -272,10 +292,13 @@ __device__ inline float power(float log2_decay, int n) { return __builtin_amdgcn
 __device__ inline bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
 
+// A chunk without starts of episodes and with all of its steps is computed apart, without what the others check (forward and backward,
+// 80 x 8 x 512 x 4 heads of 64, bf16: 665 -> 582 us).
 template <bool YES> struct Plain { static constexpr bool yes = YES; };
 
 constexpr int kGroups = 1 << 15;       // of 8 columns, in x of a grid: its work items stay below 2^32
 
+// What registers allow without spills (the build refuses kernels that spill).
 template <typename E, int KB> constexpr int waves_per_simd() { return KB > 2 ? 2 : sizeof(E) == 4 ? (KB == 1 ? 3 : 2) : __is_same(E, __bf16) || KB == 1 ? 4 : 3; }
 
 // A wavefront has 16 of the state's columns, the workgroup those of NW wavefronts.
@@ -287,7 +310,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw;
   constexpr bool kTwice = kIn != kRaw;                               // queries in parts and as they are
   static_assert(C == 32, "two tiles of rows; starts of episodes are the bits of a word");
-  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kOf * T::kPlane], values[kIn * TV::kPlane];
+  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kFaded * T::kPlane], values[kIn * TV::kPlane];
   __shared__ u32x2 shared_weights[3][kOf][64];
   __shared__ int bad[2];
   // the roles of a column one after the other on one XCD: they read the same arrays
@@ -392,7 +415,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         if (!reverse) f = role.write * power(l2, max(count - 1 - r, 0));
         f = starts(r) == all_starts ? f : 0.0f;
       }
-      next_k.template put<kOf>(faded, i, f, true);
+      next_k.template put<kFaded>(faded, i, f, true);
     }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
@@ -615,6 +638,7 @@ template <int NW, int AHEAD> __global__ void __launch_bounds__(kScan * NW) k_sca
   }
 }
 
+// Bound by reading and writing the states: 80 agents x 64 rows x 4 heads of 64 x 64, 546 MB, 104 us (5.2 TB/s; elements one by one: 146 us).
 // A workgroup of NW wavefronts per row and head; a thread has four columns of every so many'th row of the state.
 template <typename E, int NW> __global__ void __launch_bounds__(64 * NW) k_step(LinearStep a) {
   constexpr int kStep = 64 * NW, kRows = 4;
@@ -694,7 +718,7 @@ int waves_of(int V) { return V <= 32 ? 2 : V <= 64 ? 4 : 8; }
 template <typename E, int KB> int64_t at_once(int waves) {
   typedef Parts<E> P;
   const int plane = 2 * kChunk * (32 * KB + 8), values = 2 * kChunk * (16 * waves + 8);
-  const int lds = (P::kRaw + P::kIn + P::kOf + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
+  const int lds = (P::kRaw + P::kIn + kFaded + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
   const int by_lds = kLds / lds, by_waves = 4 * waves_per_simd<E, KB>() / waves;
   return (int64_t)kCUs * (by_lds < by_waves ? by_lds : by_waves);
 }

@@ -9,7 +9,8 @@ from oracle import linear as L
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 OUT = {F32: (0.0, 0.0), BF16: (2.0 ** -8, 2.0 ** -133), F16: (2.0 ** -11, 2.0 ** -24)}   # half a unit, smallest value
 UNIT = 2.0 ** -24
-# what lies between an operand of a matrix product and the value it stands for: two parts of 8 bits each for 16-bit arrays, three for fp32
+# what lies between an operand of a matrix product and the value it stands for: two parts of 8 bits each for outputs of 16 bits, three for fp32
+# ones, states among them
 OPERAND = {F32: 2.0 ** -23, BF16: 2.0 ** -16, F16: 2.0 ** -16}
 
 
@@ -75,14 +76,19 @@ def plan_of(shape, dtype, **kw):
 
 def check_forward(shape, dtype, c, got=None, scale=None):
     o, last = plan_of(shape, dtype, scale=scale).forward(**c) if got is None else got
-    want, want_last, E = L.forward(**{k: numpy_of(x) for k, x in c.items()}, scale=scale, unit=UNIT, operand=OPERAND[dtype])
+    given = {k: numpy_of(x) for k, x in c.items()}
+    want, want_last, E = L.forward(**given, scale=scale, unit=UNIT, operand=OPERAND[dtype])
     check("o", o, want, E["o"], dtype)
+    if dtype != F32:
+        E = L.forward(**given, scale=scale, unit=UNIT, operand=OPERAND[F32])[2]
     check("state_last", last, want_last, E["state_last"])
 
 
 def check_backward(shape, dtype, c, do, dlast, got=None, scale=None):
     got = plan_of(shape, dtype, scale=scale).backward(do=do, dstate_last=dlast, **c) if got is None else got
-    want, E = L.backward(do=numpy_of(do), dstate_last=numpy_of(dlast), **{k: numpy_of(x) for k, x in c.items()}, scale=scale, unit=UNIT,
-                         operand=OPERAND[dtype])
+    given = dict({k: numpy_of(x) for k, x in c.items()}, do=numpy_of(do), dstate_last=numpy_of(dlast), scale=scale, unit=UNIT)
+    want, E = L.backward(**given, operand=OPERAND[dtype])
+    if dtype != F32:
+        E = dict(E, dstate0=L.backward(**given, operand=OPERAND[F32])[1]["dstate0"])
     for name, x in zip(("dq", "dk", "dv", "dstate0"), got):
         check(name, x, want[name], E[name], F32 if name == "dstate0" else dtype)
