@@ -44,8 +44,8 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 #define POP_LDS __attribute__((address_space(3)))
 
 // Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them); a computed operand of outputs (a weight, a state) to
-// 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11 (kOf); keys times their decay to 24 bits (kFaded),
-// as states are fp32.
+// 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11 (kOf); keys times their decay to 24 bits (kFaded)
+// where the state itself is an output, as that is fp32.
 // Where both operands are arrays' values, products take them as they are where there are instructions for the type: kRaw parts.
 constexpr int kFaded = 3;
 template <typename E> struct Parts { static constexpr int kIn = 2, kOf = 2, kRaw = 1; };
@@ -284,7 +284,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     }
     return o;
   }
-  static __device__ inline Operand<kFaded> channels(unsigned short* plane, int d, int lane) { return turned<kFaded>(plane, channel_of(d, lane & 3, 0), lane); }
+  template <int N> static __device__ inline Operand<N> channels(unsigned short* plane, int d, int lane) { return turned<N>(plane, channel_of(d, lane & 3, 0), lane); }
   static __device__ inline Operand<kIn> columns(unsigned short* plane, int w, int lane) { return turned<kIn>(plane, 16 * w + 4 * (lane & 3), lane); }
 };
 
@@ -384,6 +384,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   sync_lds();
   if (tainted) bad[0] = 1;
   bool any_cut = false;
+  const bool exact = kFaded == kOf || (role.exact && (states || seg == share.segments - 1));
 
   int n = 0;
   for (; n < n_chunks; ++n) {
@@ -415,7 +416,8 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         if (!reverse) f = role.write * power(l2, max(count - 1 - r, 0));
         f = starts(r) == all_starts ? f : 0.0f;
       }
-      next_k.template put<kFaded>(faded, i, f, true);
+      if (exact) next_k.template put<kFaded>(faded, i, f, true);
+      else next_k.template put<kOf>(faded, i, f, true);
     }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
@@ -482,8 +484,16 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
 #pragma unroll
         for (int d = 0; d < 2 * KB; ++d) S[d] *= whole;
       }
+      if constexpr (kFaded > kOf) {
+        if (exact)
 #pragma unroll
-      for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::channels(faded, d, lane), value, S[d]);
+          for (int d = 0; d < 2 * KB; ++d) {
+            if constexpr (kIn > 1) S[d] = product(T::template channels<1>(faded + T::kPlane, d, lane), Operand<1>{{value.part[1]}}, S[d]);
+            S[d] = product(T::template channels<1>(faded + kOf * T::kPlane, d, lane), Operand<1>{{value.part[0]}}, S[d]);
+          }
+      }
+#pragma unroll
+      for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::template channels<kOf>(faded, d, lane), value, S[d]);
     };
     if (!states) {
       if (regular) pairs(Plain<true>());
