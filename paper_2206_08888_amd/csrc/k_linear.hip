@@ -153,15 +153,16 @@ __device__ inline int here_only(int v) {
   return v;
 }
 
-// The channel that row 4 g + i of tile d of the state stands for: tiles 2 n and 2 n + 1 share 32 channels so that what a lane has of both is
-// eight in a row, as the operands from LDS have them.
-__device__ inline int channel_of(int d, int g, int i) { return 32 * (d / 2) + 8 * g + 4 * (d % 2) + i; }
+// The channel that row 4 g + i of tile d of the state stands for.
+__device__ inline int channel_of(int d, int g, int i) { return 16 * d + 4 * g + i; }
 
 // C steps of an array's channels: the threads of the workgroup take vectors of 16 bytes in turn.  Row r of a chunk is its step r, from the
 // end in reverse.
 template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   static constexpr int kVec = 16 / sizeof(E), kAcross = 32 * KB / kVec, kAll = C * kAcross, kEach = (kAll + 64 * NW - 1) / (64 * NW);
-  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
+  // Planes that rows are read of and ones that are turned over: strides that spread a read's lanes over all banks (all planes with the first
+  // stride, forward and backward of 2 x 2 x 16383 x 4 heads of 128, fp16: 882 against 757 us).
+  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kTurned = 32 * KB + 16, kTurnedPlane = C * kTurned, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
   typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
   static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
@@ -236,18 +237,18 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
       b = (float)x[1];
     }
   }
-  static __device__ inline unsigned short* place(unsigned short* plane, int i) { return plane + row(i) * kStride + channel(i); }
+  template <bool TURNED> static __device__ inline unsigned short* place(unsigned short* plane, int i) { return plane + row(i) * (TURNED ? kTurned : kStride) + channel(i); }
   // Into LDS, part by part, or as they are.
-  template <int N> __device__ inline void store(unsigned short* plane) const {
+  template <int N, bool TURNED> __device__ inline void store(unsigned short* plane) const {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (!whole(i)) break;
-      if constexpr (N == 1) *(u32x4*)place(plane, i) = v[i];
-      else put<N>(plane, i, 1.0f, false);
+      if constexpr (N == 1) *(u32x4*)place<TURNED>(plane, i) = v[i];
+      else put<N, TURNED>(plane, i, 1.0f, false);
     }
   }
   // Vector i times f.
-  template <int N> __device__ inline void put(unsigned short* plane, int i, float f, bool times) const {
+  template <int N, bool TURNED> __device__ inline void put(unsigned short* plane, int i, float f, bool times) const {
     Word word[N];
 #pragma unroll
     for (int d = 0; d < kPairs; ++d) {
@@ -260,7 +261,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
       for (int n = 0; n < N; ++n) word[n][d] = part[n];
     }
 #pragma unroll
-    for (int n = 0; n < N; ++n) *(Word*)(place(plane, i) + n * kPlane) = word[n];
+    for (int n = 0; n < N; ++n) *(Word*)(place<TURNED>(plane, i) + n * (TURNED ? kTurnedPlane : kPlane)) = word[n];
   }
   // Rows 16 tile .. of 32 channels as an operand: a lane has channels 8 g .. 8 g + 7.
   template <int N> static __device__ inline Operand<N> rows(const unsigned short* plane, int tile, int kb, int lane) {
@@ -270,22 +271,30 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     for (int n = 0; n < N; ++n) o.part[n] = *(const u32x4*)(from + n * kPlane);
     return o;
   }
-  // Sixteen channels of 32 rows as an operand, four rows of four times four channels turned over by the read: those of half `d % 2` of block
-  // d / 2 (channel_of), and 16 w .. 16 w + 15.
-  template <int N> static __device__ inline Operand<N> turned(unsigned short* plane, int first, int lane) {
+  // The same, a lane with channels 4 g .. 4 g + 3 and 16 + 4 g .. as two tiles of the state have them.
+  template <int N> static __device__ inline Operand<N> rows_in_tiles(const unsigned short* plane, int tile, int kb, int lane) {
     Operand<N> o;
-    unsigned short* from = plane + (4 * (lane >> 4) + (lane & 15) / 4) * kStride + first;
+    const unsigned short* from = plane + (16 * tile + (lane & 15)) * kStride + 32 * kb + 4 * (lane >> 4);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kPlane));
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kPlane + 16 * kStride));
+      const u32x2 x = *(const u32x2*)(from + n * kPlane), y = *(const u32x2*)(from + n * kPlane + 16);
+      o.part[n] = u32x4{x[0], x[1], y[0], y[1]};
+    }
+    return o;
+  }
+  // Channels 16 d .. 16 d + 15 of 32 rows as an operand, four rows of four times four channels turned over by the read.
+  template <int N> static __device__ inline Operand<N> channels(unsigned short* plane, int d, int lane) {
+    Operand<N> o;
+    unsigned short* from = plane + (4 * (lane >> 4) + (lane & 15) / 4) * kTurned + channel_of(d, lane & 3, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kTurnedPlane));
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((POP_LDS s16x4*)(from + n * kTurnedPlane + 16 * kTurned));
       const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
       o.part[n] = u32x4{x[0], x[1], y[0], y[1]};
     }
     return o;
   }
-  template <int N> static __device__ inline Operand<N> channels(unsigned short* plane, int d, int lane) { return turned<N>(plane, channel_of(d, lane & 3, 0), lane); }
-  static __device__ inline Operand<kIn> columns(unsigned short* plane, int w, int lane) { return turned<kIn>(plane, 16 * w + 4 * (lane & 3), lane); }
 };
 
 __device__ inline float power(float log2_decay, int n) { return __builtin_amdgcn_exp2f((float)n * log2_decay); }
@@ -310,7 +319,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw;
   constexpr bool kTwice = kIn != kRaw;                               // queries in parts and as they are
   static_assert(C == 32, "two tiles of rows; starts of episodes are the bits of a word");
-  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kFaded * T::kPlane], values[kIn * TV::kPlane];
+  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kFaded * T::kTurnedPlane], values[kIn * TV::kTurnedPlane];
   __shared__ u32x2 shared_weights[3][kOf][64];
   __shared__ int bad[2];
   // the roles of a column one after the other on one XCD: they read the same arrays
@@ -397,13 +406,13 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     const int all_starts = __popc(cuts);
     next_k.settle(k, count, reverse);
     next_v.settle(v, count, reverse);
-    next_v.template store<kIn>(values);
+    next_v.template store<kIn, true>(values);
     bool fine = next_k.finite() & next_v.finite();
     if (!states) {
       next_q.settle(q, count, reverse);
-      next_k.template store<kRaw>(keys);
-      next_q.template store<kIn>(queries);
-      if constexpr (kTwice) next_q.template store<kRaw>(asked);
+      next_k.template store<kRaw, false>(keys);
+      next_q.template store<kIn, false>(queries);
+      if constexpr (kTwice) next_q.template store<kRaw, false>(asked);
       fine &= next_q.finite();
     }
     if (!fine) bad[n & 1] = 1;
@@ -416,8 +425,8 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         if (!reverse) f = role.write * power(l2, max(count - 1 - r, 0));
         f = starts(r) == all_starts ? f : 0.0f;
       }
-      if (exact) next_k.template put<kFaded>(faded, i, f, true);
-      else next_k.template put<kOf>(faded, i, f, true);
+      if (exact) next_k.template put<kFaded, true>(faded, i, f, true);
+      else next_k.template put<kOf, true>(faded, i, f, true);
     }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
@@ -458,7 +467,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
 #pragma unroll
       for (int d = 0; d < KB; ++d)
 #pragma unroll
-        for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::template rows<kIn>(queries, tile, d, lane), out[tile]);
+        for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::template rows_in_tiles<kIn>(queries, tile, d, lane), out[tile]);
 #pragma unroll
       for (int tile = 0; tile < 2; ++tile) {
         float f = into[tile];
@@ -488,8 +497,8 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         if (exact)
 #pragma unroll
           for (int d = 0; d < 2 * KB; ++d) {
-            if constexpr (kIn > 1) S[d] = product(T::template channels<1>(faded + T::kPlane, d, lane), Operand<1>{{value.part[1]}}, S[d]);
-            S[d] = product(T::template channels<1>(faded + kOf * T::kPlane, d, lane), Operand<1>{{value.part[0]}}, S[d]);
+            if constexpr (kIn > 1) S[d] = product(T::template channels<1>(faded + T::kTurnedPlane, d, lane), Operand<1>{{value.part[1]}}, S[d]);
+            S[d] = product(T::template channels<1>(faded + kOf * T::kTurnedPlane, d, lane), Operand<1>{{value.part[0]}}, S[d]);
           }
       }
 #pragma unroll
@@ -506,7 +515,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     // A product with a weight of zero would carry what is not finite where it does not belong: the rest goes step by step.
     if (__builtin_amdgcn_readfirstlane(not_fine) != 0) break;
     if (!idle) {
-      value = TV::columns(values, wave, lane);
+      value = TV::template channels<kIn>(values, wave, lane);
       if (regular) next_state(Plain<true>());
       else next_state(Plain<false>());
     }
@@ -727,8 +736,8 @@ int waves_of(int V) { return V <= 32 ? 2 : V <= 64 ? 4 : 8; }
 // Workgroups that the card holds at once.
 template <typename E, int KB> int64_t at_once(int waves) {
   typedef Parts<E> P;
-  const int plane = 2 * kChunk * (32 * KB + 8), values = 2 * kChunk * (16 * waves + 8);
-  const int lds = (P::kRaw + P::kIn + kFaded + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
+  const int plane = 2 * kChunk * (32 * KB + 8), turned = 2 * kChunk * (32 * KB + 16), values = 2 * kChunk * (16 * waves + 16);
+  const int lds = (P::kRaw + P::kIn + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + kFaded * turned + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
   const int by_lds = kLds / lds, by_waves = 4 * waves_per_simd<E, KB>() / waves;
   return (int64_t)kCUs * (by_lds < by_waves ? by_lds : by_waves);
 }
