@@ -15,9 +15,9 @@
 // Two barriers a chunk.
 //
 // What bounds it: at 64 x 64 in bf16 memory and the issue of instructions together (80 x 8 x 512 x 4 heads: forward 170 us where the bytes alone
-// take 131 at a large copy's rate, without memory 115 and without sums 160; three gradients 410 us, 230 at least).  At 128 x 128 in fp16 the
-// reads of operands from LDS, 1 KB for each 16 x 16 x 32 product: 720 us, forward and backward of 2 x 2 x 16383 x 4 heads.  fp32 has six
-// products for one, and 60 KB of LDS for a workgroup of 64 x 64: two on a CU.  Chunks of 64 steps need the registers of two; 32 columns a
+// take 131 at a large copy's rate, an earlier form without memory 115 and without sums 160; three gradients 420 us, 230 at least).  At 128 x
+// 128 in fp16 the reads of operands from LDS, 1 KB for each 16 x 16 x 32 product: 757 us, forward and backward of 2 x 2 x 16383 x 4 heads.
+// fp32 has six products for one, and 63 KB of LDS for a workgroup of 64 x 64: two on a CU.  Chunks of 64 steps need the registers of two; 32 columns a
 // wavefront, which would halve the reads of LDS, do not fit either.
 #include <hip/hip_runtime.h>
 #include "operators.h"

@@ -1,6 +1,7 @@
 """Operators for populations of recurrent agents on device tensors: the gated linear recurrence, linear attention with a decay
-for each head, clipping of gradients by their norm, and the orthogonalised (Muon) update.  Argument marshalling for the calls of include/pop.h of the same names; everything is computed in the
-HIP kernels of libpop.so, on PyTorch's current stream, asynchronously.
+for each head, clipping of gradients by their norm, and the orthogonalised (Muon) update.  Argument marshalling for the calls
+of include/pop.h of the same names; everything is computed in the HIP kernels of libpop.so, on PyTorch's current stream,
+asynchronously.
 
 Outputs and workspaces come from PyTorch's allocator, call by call, so calls may run on any stream and inside
 torch.cuda.graph; tensors used on another stream than their own need the usual events and record_stream.
