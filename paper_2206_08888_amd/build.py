@@ -42,6 +42,11 @@ def _run(cmd):
     return out
 
 
+def vector_spills(log):
+    """(kernel, vector registers that it spills) for every kernel of hipcc's report on their resources."""
+    return [(part.split(None, 1)[0], int(n)) for part in log.split("Function Name: ")[1:] for n in re.findall(r"VGPRs Spill: (\d+)", part)[:1]]
+
+
 def build(verbose=False, extra_flags=(), trace=False):
     os.makedirs(OBJ, exist_ok=True)
     cc = _hipcc()
@@ -54,8 +59,8 @@ def build(verbose=False, extra_flags=(), trace=False):
         if src not in WITHOUT_SPILLS:
             return _run([cc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj])
         out = _run([cc, *FLAGS, *extra_flags, "-Rpass-analysis=kernel-resource-usage", "-c", os.path.join(CSRC, src), "-o", obj])
-        used = re.findall(r"Function Name: (\S+)(?:.(?!Function Name))*?VGPRs Spill: (\d+)", out, re.S)
-        spilling = [name for name, n in used if int(n)]
+        used = vector_spills(out)
+        spilling = [name for name, n in used if n]
         if spilling or not used:
             os.remove(obj)
             raise RuntimeError("%s: kernels spill vector registers: %s" % (src, ", ".join(spilling) or "not known"))
