@@ -5,7 +5,7 @@
 //   o_i = read (lambda^(i+1) S^T q_i + write sum_{j <= i} lambda^(i-j) (k_j . q_i) v_j),    S' = lambda^32 S + write sum_j lambda^(31-j) k_j v_j^T
 //
 // and where episodes start, pairs of steps in different ones have weight 0 and the state reaches steps in front of the first start only.
-// All sums are products of 16 x 16 x 32 on the bf16 matrix instructions, operands in exact or 16 to 24 bit parts (Parts), sums in fp32.  The
+// All sums are products of 16 x 16 x 32 on the bf16 matrix instructions, operands in exact or 24 bit parts (Parts), sums in fp32.  The
 // three gradients are the same sums with other roles (op_api.hip): dq with d_o, v, k for q, k, v and the states turned over; dv and dk from
 // the end with k, q, d_o and v, d_o, q.  They go in one launch.
 //
@@ -43,14 +43,15 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 #define POP_LDS __attribute__((address_space(3)))
 
-// Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them); a computed operand of outputs (a weight, a state) to
-// 24 bits for fp32 arrays and to 16 for 16-bit ones, whose own values have 8 or 11 (kOf); keys times their decay to 24 bits (kFaded)
-// where the state itself is an output, as that is fp32.
+// Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them); a computed operand (a weight, a state, keys times
+// their decay) to 24 bits, as fp32 has it, whatever the arrays' type: states are fp32, and where sums cancel what is cut off in front of
+// the output's rounding is all that is left.  (Two parts, 16 bits, for 16-bit arrays: forward and backward of 80 x 8 x 512 x 4 heads of 64 in
+// bf16 587 us instead of 657, of 2 x 2 x 16383 x 4 heads of 128 in fp16 760 instead of 793.)
 // Where both operands are arrays' values, products take them as they are where there are instructions for the type: kRaw parts.
-constexpr int kFaded = 3;
-template <typename E> struct Parts { static constexpr int kIn = 2, kOf = 2, kRaw = 1; };
-template <> struct Parts<__bf16> { static constexpr int kIn = 1, kOf = 2, kRaw = 1; };
-template <> struct Parts<float> { static constexpr int kIn = 3, kOf = 3, kRaw = 3; };
+constexpr int kOf = 3;
+template <typename E> struct Parts { static constexpr int kIn = 2, kRaw = 1; };
+template <> struct Parts<__bf16> { static constexpr int kIn = 1, kRaw = 1; };
+template <> struct Parts<float> { static constexpr int kIn = 3, kRaw = 3; };
 
 // An operand of v_mfma_f32_16x16x32_bf16: lane l has row (or column) l % 16 and the 8 places 4 g + j and 16 + 4 g + j, j = 0 .. 3, g = l / 16,
 // of the 32 that are summed over.  Their order is free as long as both operands have the same, and in this one two results one under the
@@ -162,7 +163,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   static constexpr int kVec = 16 / sizeof(E), kAcross = 32 * KB / kVec, kAll = C * kAcross, kEach = (kAll + 64 * NW - 1) / (64 * NW);
   // Planes that rows are read of and ones that are turned over: strides that spread a read's lanes over all banks (all planes with the first
   // stride, forward and backward of 2 x 2 x 16383 x 4 heads of 128, fp16: 882 against 757 us).
-  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kTurned = 32 * KB + 16, kTurnedPlane = C * kTurned, kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
+  static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kTurned = 32 * KB + 16, kTurnedPlane = C * kTurned, kIn = Parts<E>::kIn, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
   typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
   static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
@@ -316,10 +317,10 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   typedef Tile<E, KB, NW, C, HOW> T;
   typedef Tile<E, NW / 2, NW, C, HOW> TV;
   typedef Steps<E, C, HOW> Array;
-  constexpr int kIn = Parts<E>::kIn, kOf = Parts<E>::kOf, kRaw = Parts<E>::kRaw;
+  constexpr int kIn = Parts<E>::kIn, kRaw = Parts<E>::kRaw;
   constexpr bool kTwice = kIn != kRaw;                               // queries in parts and as they are
   static_assert(C == 32, "two tiles of rows; starts of episodes are the bits of a word");
-  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kFaded * T::kTurnedPlane], values[kIn * TV::kTurnedPlane];
+  __shared__ __attribute__((aligned(16))) unsigned short keys[kRaw * T::kPlane], queries[kIn * T::kPlane], asked[kTwice ? kRaw * T::kPlane : 8], faded[kOf * T::kTurnedPlane], values[kIn * TV::kTurnedPlane];
   __shared__ u32x2 shared_weights[3][kOf][64];
   __shared__ int bad[2];
   // the roles of a column one after the other on one XCD: they read the same arrays
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   const int len = a.lengths ? min(max(a.lengths[row], 0), a.T) : a.T;
   const uint8_t* reset = a.reset.data ? (const uint8_t*)a.reset.data + p * a.reset.agent + b * a.reset.row : nullptr;
   const float l2 = log_decay_of(a.log_decay, p * a.H + h) * 1.44269504f, lambda = power(l2, 1);
-  const int before = reverse ? 0 : 1, behind = reverse ? 1 : 0;     // factors of the state on its way in and out, beside those between rows
+  const int behind = reverse ? 1 : 0;                               // factors of the state on its way out, beside those between rows (on its way in: 1 - behind)
   const int segment = reverse ? share.segments - 1 - seg : seg, from = min(segment * share.per, share.chunks), until = min(from + share.per, share.chunks);
   const int start = from * C, end = min(until * C, a.T), n_chunks = max(0, (min(end, len) - start + C - 1) / C);
   const int first_t = start + (reverse ? max(n_chunks - 1, 0) * C : 0);
@@ -364,11 +365,9 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
     tainted = any_lane(tainted);
   }
 
-  // Weights of the state on its way in, and of this thread's rows of keys on their way out.
+  // Weights of this thread's rows of keys on their way out.
   const float both = role.read * role.write, whole = power(l2, C);
-  float into[2], outof[T::kEach];
-#pragma unroll
-  for (int n = 0; n < 2; ++n) into[n] = role.read * power(l2, 16 * n + at + before);
+  float outof[T::kEach];
 #pragma unroll
   for (int i = 0; i < T::kEach; ++i) outof[i] = role.write * power(l2, max(C - 1 - T::row(i), 0) + behind);
 
@@ -393,7 +392,6 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
   sync_lds();
   if (tainted) bad[0] = 1;
   bool any_cut = false;
-  const bool exact = kFaded == kOf || (role.exact && (states || seg == share.segments - 1));
 
   int n = 0;
   for (; n < n_chunks; ++n) {
@@ -425,8 +423,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         if (!reverse) f = role.write * power(l2, max(count - 1 - r, 0));
         f = starts(r) == all_starts ? f : 0.0f;
       }
-      if (exact) next_k.template put<kFaded, true>(faded, i, f, true);
-      else next_k.template put<kOf, true>(faded, i, f, true);
+      next_k.template put<kOf, true>(faded, i, f, true);
     }
     sync_lds();
     if (n + 1 < n_chunks) load(n + 1);
@@ -470,11 +467,8 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         for (int tile = 0; tile < 2; ++tile) out[tile] = product(memory[d], T::template rows_in_tiles<kIn>(queries, tile, d, lane), out[tile]);
 #pragma unroll
       for (int tile = 0; tile < 2; ++tile) {
-        float f = into[tile];
-        if constexpr (!plain.yes) {
-          if (reverse) f = role.read * power(l2, max(16 * tile + here_only(at) - (C - count), 0));
-        }
-        out[tile] *= f;
+        const int i = 16 * tile + here_only(at);                     // (found again: a register that the bf16 kernels do not have)
+        out[tile] *= role.read * power(l2, reverse ? max(i - (C - count), 0) : i + 1);
         if constexpr (!plain.yes) {
           const bool own = starts(16 * tile + at) != 0;              // nothing of the state
 #pragma unroll
@@ -492,14 +486,6 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
       } else {
 #pragma unroll
         for (int d = 0; d < 2 * KB; ++d) S[d] *= whole;
-      }
-      if constexpr (kFaded > kOf) {
-        if (exact)
-#pragma unroll
-          for (int d = 0; d < 2 * KB; ++d) {
-            if constexpr (kIn > 1) S[d] = product(T::template channels<1>(faded + T::kTurnedPlane, d, lane), Operand<1>{{value.part[1]}}, S[d]);
-            S[d] = product(T::template channels<1>(faded + kOf * T::kTurnedPlane, d, lane), Operand<1>{{value.part[0]}}, S[d]);
-          }
       }
 #pragma unroll
       for (int d = 0; d < 2 * KB; ++d) S[d] = product(T::template channels<kOf>(faded, d, lane), value, S[d]);
@@ -737,7 +723,7 @@ int waves_of(int V) { return V <= 32 ? 2 : V <= 64 ? 4 : 8; }
 template <typename E, int KB> int64_t at_once(int waves) {
   typedef Parts<E> P;
   const int plane = 2 * kChunk * (32 * KB + 8), turned = 2 * kChunk * (32 * KB + 16), values = 2 * kChunk * (16 * waves + 16);
-  const int lds = (P::kRaw + P::kIn + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + kFaded * turned + P::kIn * values + 3 * P::kOf * 64 * 8 + 64;
+  const int lds = (P::kRaw + P::kIn + (P::kIn != P::kRaw ? P::kRaw : 0)) * plane + kOf * turned + P::kIn * values + 3 * kOf * 64 * 8 + 64;
   const int by_lds = kLds / lds, by_waves = 4 * waves_per_simd<E, KB>() / waves;
   return (int64_t)kCUs * (by_lds < by_waves ? by_lds : by_waves);
 }

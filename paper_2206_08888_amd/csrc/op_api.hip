@@ -408,7 +408,7 @@ int pop_linear_forward(const pop_linear_config* cfg, const pop_linear_io* io, vo
   if ((rc = check_apart(r)) != POP_OK) return rc;
   LinearArgs a = linear_args(cfg, io);
   a.roles = 1;
-  a.role[0] = {io->q, io->k, io->v, io->o, cfg->key_dim, cfg->value_dim, 0, cfg->scale, 1.0f, io->state0, cfg->value_dim, 1, 1, io->state_last};
+  a.role[0] = {io->q, io->k, io->v, io->o, cfg->key_dim, cfg->value_dim, 0, cfg->scale, 1.0f, io->state0, cfg->value_dim, 1, io->state_last};
   return launched(launch_linear(a, cfg->dtype, workspace, (hipStream_t)hip_stream));
 }
 
@@ -444,9 +444,9 @@ int pop_linear_backward(const pop_linear_config* cfg, const pop_linear_io* io, c
   const float scale = cfg->scale;
   const int k = (int)K, v = (int)V;
   a.roles = 3;
-  a.role[0] = {grads->d_o, io->v, io->k, grads->dq, v, k, 0, scale, 1.0f, io->state0, 1, v, 0, nullptr};
-  a.role[1] = {io->k, io->q, grads->d_o, grads->dv, k, v, 1, 1.0f, scale, grads->dstate_last, v, 1, 1, grads->dstate0};
-  a.role[2] = {io->v, grads->d_o, io->q, grads->dk, v, k, 1, 1.0f, scale, grads->dstate_last, 1, v, 0, nullptr};
+  a.role[0] = {grads->d_o, io->v, io->k, grads->dq, v, k, 0, scale, 1.0f, io->state0, 1, v, nullptr};
+  a.role[1] = {io->k, io->q, grads->d_o, grads->dv, k, v, 1, 1.0f, scale, grads->dstate_last, v, 1, grads->dstate0};
+  a.role[2] = {io->v, grads->d_o, io->q, grads->dk, v, k, 1, 1.0f, scale, grads->dstate_last, 1, v, nullptr};
   return launched(launch_linear(a, cfg->dtype, workspace, (hipStream_t)hip_stream));
 }
 

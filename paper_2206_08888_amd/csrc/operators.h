@@ -48,7 +48,6 @@ struct LinearRole {
   float read, write;
   const float* first;                // or NULL: zeros.  Element [i, j] of a state at i * first_k + j * first_v
   int first_k, first_v;
-  int exact;                         // the last state is an output, asked for or not: no bit of the others hangs on that
   float* last;                       // [i, j] at i * V + j; in reverse the gradient in front of step 0; or NULL
 };
 struct LinearArgs {
