@@ -417,10 +417,13 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  *
  * with S_{-1} = state0 and, where reset_t is not zero, 0 in place of S_{t-1}.  Steps from a sequence's length on are not used;
  * o is 0 there and so are the gradients.  States and sums are fp32 whatever the arrays' type.  An infinity or a NaN reaches the steps
- * that the formula lets it reach and no others: not earlier ones, and none behind a reset.  Steps are summed in groups, which takes
- * scale * (k_s . q_t) of steps up to 32 apart: beyond fp32's range it is an infinity even where the state's products are not.
+ * that the formula lets it reach and no others: not earlier ones, and none behind a reset.  S_t^T q_t is summed in front of its scaling.
  *
- * POP_EUNSUPPORTED: key_dim or value_dim beyond 128, T beyond 2^22, P * batch * heads from 2^24 on. */
+ * Steps are summed in groups of 32, which takes k_s . q_t (backward v_s . d_o_t too): what of these is below fp32's range is lost, whatever
+ * it is multiplied with.  From values of about 2^60 on in q or k (v or d_o), less by the root of a scale above 1, the rest of a sequence
+ * goes step by step, which is slower, so that nothing leaves fp32's range that the formula's own states and sums keep within it.
+ *
+ * POP_EUNSUPPORTED: key_dim or value_dim beyond 128, T beyond 2^22, P * batch * heads from 2^24 on, a scale beyond 2^80 for fp16 arrays. */
 enum { POP_LINEAR_MAX_DIM = 128 };
 typedef struct {
   int32_t P, batch;              /* agents, sequences of each agent */

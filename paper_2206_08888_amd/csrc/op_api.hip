@@ -17,6 +17,8 @@ constexpr int64_t kMaxWorkgroups = 1 << 21;  // of one layer's matrices
 constexpr int64_t kMaxLinearRows = 1 << 24;  // P * batch * heads: 256 work items each
 constexpr int64_t kMaxElements = 1ll << 40, kMaxPieces = 1 << 24;
 
+constexpr float kMostScale = 0x1p80f;        // times products of fp16 values over 128 channels (2^39): in fp32's range
+
 constexpr double kMostSingular = 8.0;
 
 int64_t element_bytes(int32_t dtype) { return dtype == POP_F32 ? 4 : 2; }
@@ -215,6 +217,7 @@ int check_linear(const pop_linear_config* c) {
     return fail_thread(POP_EINVAL, "config: P, batch, heads, key_dim and value_dim must be positive, T not negative");
   if (c->dtype != POP_F32 && c->dtype != POP_BF16 && c->dtype != POP_F16) return fail_thread(POP_EINVAL, "config: unknown dtype %d", c->dtype);
   if (!isfinite(c->scale)) return fail_thread(POP_EINVAL, "config: scale is not finite");
+  if (c->dtype == POP_F16 && fabsf(c->scale) > kMostScale) return fail_thread(POP_EUNSUPPORTED, "scale must be at most 2^80 for fp16 arrays");
   if (c->key_dim > POP_LINEAR_MAX_DIM || c->value_dim > POP_LINEAR_MAX_DIM)
     return fail_thread(POP_EUNSUPPORTED, "key_dim and value_dim must be at most %d", (int)POP_LINEAR_MAX_DIM);
   if (c->T > kMaxSteps) return fail_thread(POP_EUNSUPPORTED, "T must be at most %d", kMaxSteps);

@@ -52,6 +52,7 @@ struct LinearRole {
 };
 struct LinearArgs {
   int P, B, T, H;
+  unsigned border;                   // (of the launch wrapper) what keys and queries stay below so that their products are in fp32's range
   const float* log_decay;            // [P, H] or NULL: zeros
   pop_sequence reset;
   const int32_t* lengths;
