@@ -445,7 +445,8 @@ __global__ void __launch_bounds__(8192 / N, 2) k_backward(RecurArgs a, int chunk
   __shared__ float quarter[4][2][kColumns];
   const int64_t n = (int64_t)a.P * a.B * a.C;
   const Place place = place_of<MODE>(a, n, segments, true);
-  const int at = threadIdx.x % S::kLanes, run = threadIdx.x / S::kLanes, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int at = threadIdx.x % S::kLanes, run = threadIdx.x / S::kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));      // threadIdx.x would be kept in a register for the end
   const Lane l = lane_at(a, place.first + at * V);
   const int k0 = place.seg * per, k1 = MODE == kChain ? k0 + 1 : min(k0 + per, chunks);
   float bias[V];
@@ -458,7 +459,9 @@ __global__ void __launch_bounds__(8192 / N, 2) k_backward(RecurArgs a, int chunk
     g.load(a.g, l, t, a.T);
     x.load(a.x, l, t, a.T);
     dy.load(a.dy, l, t, a.T);
-    starts.load(a, l, t);
+    Lane again = l;                                            // where resets begin is found again: the 16-bit kernels of single elements have no
+    asm volatile("" : "+v"(again.p), "+v"(again.b));           // registers left for it (256; 80 agents of 8 x 512 x 129, bf16, with resets: spilled 181 us, so 171)
+    starts.load(a, again, t);
   };
   fetch(k1 - 1);
   // a column per lane: wavefront 0 carries the gradient from tile to tile, wavefront 1 takes states from `states`
