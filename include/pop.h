@@ -539,8 +539,8 @@ int pop_muon_step(const pop_ns_config* cfg, int32_t P, int32_t n_layers, const p
  *   norm_i = sqrt(sum g^2),   out = f_i g,   f_i = 1 where norm_i + eps <= max_norm_i, else max_norm_i / (norm_i + eps)
  *
  * Squares are summed in fp64, in an order that sizes alone decide; f_i is fp32, the product is rounded to fp32, and from there to the
- * type of 16-bit tensors.  A norm that is infinite or
- * NaN is reported as it is, and the formula passes it on to the agent's gradients; other agents' are not touched by it.
+ * type of 16-bit tensors.  A norm that is infinite or NaN is reported as it is, and the formula passes it on to the agent's gradients;
+ * other agents' are not touched by it.
  * POP_EUNSUPPORTED: rows * cols beyond 2^40 for an agent's part of a tensor, 2^24 or more pieces of 2^13 elements in a call. */
 enum { POP_CLIP_MAX_TENSORS = 256 };
 

@@ -180,6 +180,11 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   u32x4 v[kEach];
   static __device__ inline bool whole(int i) { return kAll % (64 * NW) == 0 || row(i) < C; }
   static __device__ inline int row(int i, int thread = threadIdx.x) { return (thread + i * 64 * NW) / kAcross; }
+  // The step of the chunk that a vector is of: not in front of the array for threads behind the last row either.
+  static __device__ inline int step(int i, bool reverse, int thread) {
+    const int m = reverse ? C - 1 - row(i, thread) : row(i, thread);
+    return kAll % (64 * NW) == 0 ? m : max(m, 0);
+  }
   static __device__ inline int channel(int i, int thread = threadIdx.x) { return (thread + i * 64 * NW) % kAcross * kVec; }
   static __device__ inline int thread() { return HOW == kWide ? (int)threadIdx.x : here_only(threadIdx.x); }
   __device__ inline void load(const Steps<E, C, HOW>& a, int n, bool reverse) {
@@ -187,7 +192,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     const int id = thread();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int m = reverse ? C - 1 - row(i, id) : row(i, id);
+      const int m = step(i, reverse, id);
       if constexpr (HOW == kWide) {
         v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, a.offset(m, channel(i, id)), 0, 0);
       } else {
@@ -209,7 +214,7 @@ template <typename E, int KB, int NW, int C, int HOW> struct Tile {
     const int id = thread();
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int m = reverse ? C - 1 - row(i, id) : row(i, id), off = max(0, channel(i, id) - (a.width - kVec)) * (int)sizeof(E) * 8;
+      const int m = step(i, reverse, id), off = max(0, channel(i, id) - (a.width - kVec)) * (int)sizeof(E) * 8;
       uint64_t lo = v[i][0] | (uint64_t)v[i][1] << 32, hi = v[i][2] | (uint64_t)v[i][3] << 32;
       if (off >= 64) {
         lo = hi;
