@@ -14,11 +14,13 @@
 // all; each wavefront holds 16 columns of S in registers, as sums of the matrix instructions that are operands of the next ones as they are.
 // Two barriers a chunk.
 //
-// What bounds it: at 64 x 64 in bf16 memory and the issue of instructions together (80 x 8 x 512 x 4 heads: forward 170 us where the bytes alone
-// take 131 at a large copy's rate, an earlier form without memory 115 and without sums 160; three gradients 420 us, 230 at least).  At 128 x
-// 128 in fp16 the reads of operands from LDS, 1 KB for each 16 x 16 x 32 product: 757 us, forward and backward of 2 x 2 x 16383 x 4 heads.
-// fp32 has six products for one, and 63 KB of LDS for a workgroup of 64 x 64: two on a CU.  Chunks of 64 steps need the registers of two; 32 columns a
-// wavefront, which would halve the reads of LDS, do not fit either.
+// What bounds it: at 64 x 64 in bf16 the issue of vector instructions, most of which split operands (80 x 8 x 512 x 4 heads: forward 179 us where
+// the bytes alone take 139 at a large copy's rate, vector instructions issue in 73 % of a CU's busy cycles, LDS works in 43 %, matrix units in
+// 23 %; three gradients 484 us, 237 at least, 80 / 49 / 26 %).  At 128 x 128 in fp16 nothing is busy half of the time (three gradients of 2 x 2 x 16383 x 4
+// heads 488 us, 45 / 39 / 29 %): 85 KB of LDS are one workgroup on a CU, two wavefronts on a SIMD, which wait 40 % of their time, as a chunk is
+// staged, a barrier, products, a barrier and outputs one after the other.  So are fp32 (six products for one, 63 KB of LDS for 64 x 64, two
+// workgroups on a CU) and few columns, where a wavefront waits 35 to 40 %.  Chunks of 64 steps need the registers of two; 32 columns
+// a wavefront, which would halve the reads of LDS, do not fit either.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <algorithm>
@@ -48,7 +50,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 // Operands of a product are sums of bf16 parts: an array's values exactly (kIn of them); a computed operand (a weight, a state, keys times
 // their decay) to 24 bits, as fp32 has it, whatever the arrays' type: states are fp32, and where sums cancel what is cut off in front of
 // the output's rounding is all that is left.  (Two parts, 16 bits, for 16-bit arrays: forward and backward of 80 x 8 x 512 x 4 heads of 64 in
-// bf16 587 us instead of 657, of 2 x 2 x 16383 x 4 heads of 128 in fp16 760 instead of 793.)
+// bf16 587 us instead of 655, of 2 x 2 x 16383 x 4 heads of 128 in fp16 760 instead of 790.)
 // Where both operands are arrays' values, products take them as they are where there are instructions for the type: kRaw parts.
 constexpr int kOf = 3;
 template <typename E> struct Parts { static constexpr int kIn = 2, kRaw = 1; };
@@ -174,7 +176,7 @@ __device__ inline int channel_of(int d, int g, int i) { return 16 * d + 4 * g + 
 template <typename E, int KB, int NW, int C, int HOW> struct Tile {
   static constexpr int kVec = 16 / sizeof(E), kAcross = 32 * KB / kVec, kAll = C * kAcross, kEach = (kAll + 64 * NW - 1) / (64 * NW);
   // Planes that rows are read of and ones that are turned over: strides that spread a read's lanes over all banks (all planes with the first
-  // stride, forward and backward of 2 x 2 x 16383 x 4 heads of 128, fp16: 882 against 757 us).
+  // stride, forward and backward of 2 x 2 x 16383 x 4 heads of 128, fp16: 816 against 787 us).
   static constexpr int kStride = 32 * KB + 8, kPlane = C * kStride, kTurned = 32 * KB + 16, kTurnedPlane = C * kTurned, kIn = Parts<E>::kIn, kRaw = Parts<E>::kRaw, kPairs = kVec / 2;
   typedef unsigned Word __attribute__((ext_vector_type(kPairs)));    // a vector's values, one part of each
   u32x4 v[kEach];
@@ -318,8 +320,8 @@ __device__ inline float power(float log2_decay, int n) { return __builtin_amdgcn
 __device__ inline bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 __device__ inline bool any_lane(bool v) { return __builtin_amdgcn_ballot_w64(v) != 0; }
 
-// A chunk without starts of episodes and with all of its steps is computed apart, without what the others check (forward and backward,
-// 80 x 8 x 512 x 4 heads of 64, bf16: 665 -> 582 us).
+// A chunk without starts of episodes and with all of its steps is computed apart, without what the others check (forward and backward of 2 x 2 x
+// 16383 x 4 heads of 128, fp16: 805 -> 787 us; of 80 x 8 x 512 x 4 heads of 64, bf16: 655 -> 650).
 template <bool YES> struct Plain { static constexpr bool yes = YES; };
 
 constexpr int kGroups = 1 << 15;       // of 8 columns, in x of a grid: its work items stay below 2^32
