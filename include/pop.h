@@ -419,8 +419,8 @@ int pop_recurrence_step(const pop_recurrence_config* cfg, const pop_recurrence_i
  * o is 0 there and so are the gradients.  States and sums are fp32 whatever the arrays' type.  An infinity or a NaN reaches the steps
  * that the formula lets it reach and no others: not earlier ones, and none behind a reset.  S_t^T q_t is summed in front of its scaling.
  *
- * Steps are summed in groups of 32, which takes k_s . q_t (backward v_s . d_o_t too): what of these is below fp32's range is lost, whatever
- * it is multiplied with.  From values of about 2^60 on in q or k (v or d_o), less by the root of a scale above 1, the rest of a sequence
+ * Steps are summed in groups of 32, which takes k_s . q_t (backward v_s . d_o_t, scale * q_t and scale * d_o_t too): what of these is below
+ * fp32's range is lost, whatever it is multiplied with.  From values of about 2^60 on in q or k (v or d_o), less by the root of a scale above 1, the rest of a sequence
  * goes step by step, which is slower, so that nothing leaves fp32's range that the formula's own states and sums keep within it.
  *
  * POP_EUNSUPPORTED: key_dim or value_dim beyond 128, T beyond 2^22, P * batch * heads from 2^24 on, a scale beyond 2^80 for fp16 arrays. */

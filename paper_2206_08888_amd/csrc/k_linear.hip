@@ -90,7 +90,8 @@ template <int N> __device__ inline Operand<N> operand(const f32x4& lo, const f32
   }
   return o;
 }
-// c + a b: all products of parts but those below the last part's rounding.
+// c + a b.  Parts that were cut off are below 2^-7 and 2^-15 of the value; of their products the ones below 2^-22 are left out: 2^-24 of a b on
+// the average, as much as a product in fp32 is rounded by, and 2^-21 at most (nothing where one operand is a single part).
 template <int A, int B> __device__ inline f32x4 product(const Operand<A>& a, const Operand<B>& b, f32x4 c) {
   constexpr int N = A > B ? A : B;
 #pragma unroll
@@ -571,7 +572,7 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
       const int64_t s = reverse ? first + behind - 1 - i : i;
       const bool cut = reset && (!reverse || s + 1 < len) && reset[(s + (reverse ? 1 : 0)) * a.reset.step];
       any_cut |= cut;
-      const float vr = column < V ? (float)vs[s * role.v.step + column] * role.write : 0.0f;
+      const float vr = column < V ? (float)vs[s * role.v.step + column] : 0.0f;
       float sum = 0.0f;
 #pragma unroll
       for (int d = 0; d < 2 * KB; ++d)
@@ -579,7 +580,11 @@ __global__ void __launch_bounds__(64 * NW, (waves_per_simd<E, KB>())) k_chunks(L
         for (int i = 0; i < 4; ++i) {
           const int kr = channel_of(d, g, i);
           if (kr < K) {
-            const float x = fmaf((float)ks[s * role.k.step + kr], vr, cut ? 0.0f : reverse ? S[d][i] : lambda * S[d][i]);
+            // the smaller one of the two times a factor above 1, the larger one times one below: within the range where all three are (fp16
+            // values times their scales always are)
+            const float key = (float)ks[s * role.k.step + kr];
+            const bool on_key = !__is_same(E, _Float16) && (fabsf(key) < fabsf(vr)) == (fabsf(role.write) > 1.0f);
+            const float x = fmaf(on_key ? key * role.write : key, on_key ? vr : vr * role.write, cut ? 0.0f : reverse ? S[d][i] : lambda * S[d][i]);
             if (!states) sum = fmaf((float)qs[s * role.q.step + kr], x, sum);
             S[d][i] = reverse ? lambda * x : x;
           }

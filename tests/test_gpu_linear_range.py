@@ -54,3 +54,15 @@ def test_values_next_to_the_border(size, dtype):
 def test_large_scales(scale, v, do, dtype):
     """scale * (k . q) within the range, and beyond it at ordinary keys and queries."""
     _case((1, 1, 70, 1, 12, 20), dtype, scale, v=v, do=do)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_large_scale_step_by_step(dtype):
+    """scale * do beyond the range where scale * q * do is not, in a sequence that one large query sends step by step."""
+    shape, scale, at = (1, 1, 100, 1, 12, 20), 2.0 ** 80, slice(80, 81)
+    c, do, dlast = make(shape, dtype, seed=9, reset=0.01)
+    c["q"], c["k"], do = ((x.double() * size).to(dtype) for x, size in ((c["q"], 2.0 ** -60), (c["k"], 2.0 ** -20), (do, 2.0 ** 60)))
+    c["q"][:, :, at] = (c["q"][:, :, at].double() * 2.0 ** 85).to(dtype)
+    do[:, :, at] = (do[:, :, at].double() * 2.0 ** -85).to(dtype)
+    check_forward(shape, dtype, c, scale=scale)
+    check_backward(shape, dtype, c, do, dlast, scale=scale)
