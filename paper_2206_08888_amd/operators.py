@@ -199,7 +199,7 @@ class LinearAttention(_Operator):
     q, k [P, batch, T', heads, key_dim], v, o [P, batch, T', heads, value_dim] and their gradients are of `dtype`, T' <= T, any
     strides with adjacent channels; both widths at most 128.  log_decay [P, heads] (at most 0; None: nothing decays) and the states
     state0, state_last, dstate_last, dstate0 [P, batch, heads, key_dim, value_dim] are float32; reset and lengths as in Recurrence.
-    scale: by default key_dim ** -0.5."""
+    scale: by default key_dim ** -0.5; for float16 at most 2 ** 80."""
 
     def __init__(self, P, batch, T, heads, key_dim, value_dim, dtype=torch.float32, device="cuda", scale=None):
         super().__init__(dtype, device)
